@@ -22,7 +22,7 @@
  * the keys (row j = column j of the paper's W_A), V[N,d] the values (row j of W_B), Wg[n_blocks,d]
  * the router.  Block b owns the contiguous neurons [b*block_size, (b+1)*block_size).
  * Ties in both selections go to the lower index; +0 and -0 tie.  The router score only selects
- * (no gate multiply), so there is no router gradient.
+ * (no gate multiply), so the layer itself gives the router no gradient; the balance loss below does.
  *
  * Conventions for every entry point
  *  - All tensor pointers are DEVICE pointers owned by the caller, row-major, contiguous, 16-byte
@@ -315,6 +315,158 @@ typedef struct {
  */
 meft_status meft_adam_rows(const meft_shape* shape, const meft_adam* hp, void* W, const void* G, float* m, float* v,
                            float* master, const int32_t* touched, const int32_t* n_touched, void* stream);
+
+/*
+ * ---- The calls around the layer in a training or serving step ---------------------------------------------------------
+ *
+ * A block of a network computes h = norm(x), routes and runs the sparse layer on h, and adds its output to the stream, usually
+ * behind dropout: y = x + dropout(out).  The calls below are these pieces, their backward passes, and what trains the router:
+ * its balance loss and its gradient.  A step of one layer:
+ *
+ *   meft_norm_fwd -> meft_route_scores -> meft_sparse_fwd -> meft_dropout_add      meft_balance_fwd
+ *   meft_dropout_add (on dy) -> meft_sparse_bwd -> meft_balance_bwd -> meft_route_bwd (adds to dh) -> meft_norm_bwd
+ *
+ * Between two layers meft_add_norm_fwd / meft_add_norm_bwd do dropout, residual add and the next norm in one pass.
+ *
+ * They follow the conventions above.  shape gives T, d, n_blocks, top_e and dtype; every other field has to be valid and is
+ * not used, flags included: all operands are device memory.  `ws` is a device workspace of meft_block_workspace_bytes(shape)
+ * bytes, 256-byte aligned; nothing in it outlives a call.  No call allocates, synchronises or uses floating-point atomics:
+ * results are identical from run to run, and every call can be captured into a HIP graph.  All sums are accumulated in fp32, and each
+ * result is rounded once, when it is stored.  Outputs must not overlap inputs except where it is said.  [T, d] operands are
+ * 16-byte aligned; so are [d] and [T, n_blocks] ones; the others need the alignment of their type.
+ * With T == 0 nothing is read but the outputs that are sums over tokens are written (zeros).
+ */
+size_t meft_block_workspace_bytes(const meft_shape* shape);
+
+typedef enum {
+  MEFT_NORM_LAYER = 0, /* mean subtracted */
+  MEFT_NORM_RMS = 1    /* root mean square only: mu = 0 */
+} meft_norm_kind;
+
+typedef struct {
+  int32_t kind; /* meft_norm_kind */
+  float eps;    /* >= 0, finite */
+} meft_norm;
+
+/*
+ * Dropout whose mask is never stored: an element stays or goes by its place alone, so the backward pass calls for the same
+ * mask again.  Element (t, c) takes 16 bits of Philox4x32 with 10 rounds, counter (c / 8, t, low word, high word of offset),
+ * key (low word, high word of seed): word (c % 8) / 2 of the result, its low half for even c; it stays where they are at least
+ * round(65536 p), and is then multiplied by 65536 / (65536 - round(65536 p)).  The mask of a token does not depend on T or d.
+ * offset: one value for each layer and step, so that masks differ; where `step` (device memory, 8-byte aligned, may be NULL) is
+ * given, the value it holds when the kernel runs is added to offset (modulo 2^64): a captured step draws anew when the program
+ * changes it between replays.  p in [0, 1) and round(65536 p) <= 65535; below 2^-17 nothing is dropped.
+ */
+typedef struct {
+  float p;
+  uint64_t seed, offset;
+} meft_drop;
+
+/*
+ * h[t, :] = (x[t, :] - mu) r gamma + beta,  mu = mean of x[t, :] (0 for the rms kind),  r = 1 / sqrt(mean (x[t, :] - mu)^2 + eps)
+ *   x, h         [T, d]     in, out; h may be x
+ *   gamma, beta  [d]        in; of dtype; beta may be NULL (no shift)
+ *   mean, rstd   [T] f32    out: mu and r for the backward; each may be NULL.  mean is 0 for the rms kind.
+ */
+meft_status meft_norm_fwd(const meft_shape* shape, const meft_norm* norm, const void* x, const void* gamma, const void* beta,
+                          void* h, float* mean, float* rstd, void* stream);
+
+/*
+ * Backward of meft_norm_fwd: with g = dh gamma, xh = (x - mu) r,
+ *   dx = r (g - mean(g) [layer kind] - xh mean(g xh)) + dy,   dgamma = sum_t dh xh,   dbeta = sum_t dh
+ *   x, gamma, mean, rstd   in   as in and from the forward; mean is not read for the rms kind and may then be NULL
+ *   dh       [T, d]   in   gradient with respect to h
+ *   dy       [T, d]   in   gradient that reaches x past the norm (the residual stream's), added to dx; may be NULL
+ *   dx       [T, d]   out  may be dh or dy
+ *   dgamma, dbeta [d] out  of dtype; both may be NULL (frozen weights), dbeta alone too; dbeta without dgamma is an
+ *                          MEFT_ERR_INVALID_ARG
+ */
+meft_status meft_norm_bwd(const meft_shape* shape, const meft_norm* norm, const void* x, const void* gamma, const float* mean,
+                          const float* rstd, const void* dh, const void* dy, void* dx, void* dgamma, void* dbeta, void* ws,
+                          size_t ws_bytes, void* stream);
+
+/*
+ * y = res + dropout(out).  The same call is its own backward: dout = dropout(dy) with res NULL (the gradient of res is dy).
+ *   drop     NULL: no dropout (serving)
+ *   out, res [T, d]   in; res may be NULL (0)
+ *   y        [T, d]   out; may be out or res
+ */
+meft_status meft_dropout_add(const meft_shape* shape, const meft_drop* drop, const uint64_t* step, const void* out, const void* res,
+                             void* y, void* stream);
+
+/*
+ * meft_dropout_add and meft_norm_fwd on its result in one pass: y = res + dropout(out), h = norm(y).  The norm is of y as it is
+ * stored, so the results are those of the two calls.  y may be out or res; h may be out or res if y is not the same.  res is required.
+ */
+meft_status meft_add_norm_fwd(const meft_shape* shape, const meft_norm* norm, const meft_drop* drop, const uint64_t* step,
+                              const void* out, const void* res, const void* gamma, const void* beta, void* y, void* h, float* mean,
+                              float* rstd, void* stream);
+
+/*
+ * Backward of meft_add_norm_fwd.  y is the forward's; dy (may be NULL) the gradient that reaches y past the norm.
+ *   dres [T, d]   out  gradient of res: the norm's backward of dh, plus dy; may be dh or dy
+ *   dout [T, d]   out  dropout(dres), taken before dres is rounded; may be dh or dy if dres is not the same
+ */
+meft_status meft_add_norm_bwd(const meft_shape* shape, const meft_norm* norm, const meft_drop* drop, const uint64_t* step,
+                              const void* y, const void* gamma, const float* mean, const float* rstd, const void* dh, const void* dy,
+                              void* dres, void* dout, void* dgamma, void* dbeta, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * meft_route, and the scores that it selects by, for the calls below: the same kernels and results.
+ *   scores [T, n_blocks] f32  out  router scores, bias included
+ *   ws     a workspace of meft_workspace_bytes(shape) bytes, as for meft_route
+ */
+meft_status meft_route_scores(const meft_shape* shape, const void* h, const void* Wg, const float* bias, int32_t* block_idx,
+                              float* block_score, float* scores, void* ws, size_t ws_bytes, void* stream);
+
+/* Weights of the two terms of the router's loss; finite. */
+typedef struct {
+  float balance, z;
+} meft_balance;
+
+/*
+ * The router's balance loss and how many tokens each block gets.  Over the n valid tokens, with P[t, :] = softmax(scores[t, :])
+ * and lse_t = log sum_b exp(scores[t, b]):
+ *   counts_b = entries of block_idx that are b,   L = n_blocks sum_b (counts_b / (n top_e)) (1/n) sum_t P[t, b],
+ *   Z = (1/n) sum_t lse_t^2,                       loss = balance L + z Z
+ * L is 1 where tokens or probabilities are spread evenly.  A score may be -inf (a block that a bias of -inf shuts out): its
+ * probability is 0.  A token whose scores are all -inf is not valid.  With no valid token everything is 0.
+ *   scores    [T, n_blocks] f32  in
+ *   block_idx [T, top_e] i32     in   as meft_route writes it; ids outside [0, n_blocks) are not counted
+ *   valid     [T] u8             in   0 for tokens that only pad the batch, whose rows are then not read; NULL: all are valid
+ *   counts    [n_blocks] i32     out
+ *   n_valid   [1] i32            out
+ *   prob      [n_blocks] f32     out  sum over the valid tokens of P[t, b]
+ *   loss      [3] f32            out  loss, L, Z (a term of weight 0 is not part of the first)
+ * Data-parallel training adds counts and n_valid up over the ranks before the backward; the ranks' gradients then add up to
+ * that of the whole batch's loss.
+ */
+meft_status meft_balance_fwd(const meft_shape* shape, const meft_balance* balance, const float* scores, const int32_t* block_idx,
+                             const uint8_t* valid, int32_t* counts, int32_t* n_valid, float* prob, float* loss, void* ws,
+                             size_t ws_bytes, void* stream);
+
+/*
+ * Gradient of loss[0] with respect to the scores (the counts have none):
+ *   dscores[t, b] = dloss P[t, b] ((balance n_blocks / n) (f_b - sum_b' f_b' P[t, b']) + (2 z / n) lse_t),  f_b = counts_b / (n top_e)
+ *   scores, valid, counts, n_valid   in   as in and from the forward
+ *   dloss    [1] f32                 in   device; NULL: 1
+ *   dscores  [T, n_blocks] f32       out  rows of tokens that are not valid are 0; may be scores
+ */
+meft_status meft_balance_bwd(const meft_shape* shape, const meft_balance* balance, const float* scores, const int32_t* counts,
+                             const int32_t* n_valid, const uint8_t* valid, const float* dloss, float* dscores, void* stream);
+
+/*
+ * The router's backward, from any gradient of its scores:
+ *   dh[t, :] = add[t, :] + sum_b dscores[t, b] Wg[b, :],   dWg[b, :] = sum_t dscores[t, b] h[t, :],   dbias[b] = sum_t dscores[t, b]
+ *   h, Wg    in   as in meft_route
+ *   add      [T, d]        in   the gradient that h has from elsewhere (meft_sparse_bwd's dh); NULL: 0
+ *   dh       [T, d]        out  may be add; may be NULL
+ *   dWg      [n_blocks, d] out  may be NULL
+ *   dbias    [n_blocks] f32 out may be NULL
+ * bf16 shapes split dscores into two bf16 parts and multiply both, so that rounding it does not show next to the result's.
+ */
+meft_status meft_route_bwd(const meft_shape* shape, const void* h, const void* Wg, const float* dscores, const void* add, void* dh,
+                           void* dWg, float* dbias, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Measurement aid (not part of the paper's method): a plain streaming copy of `bytes` bytes

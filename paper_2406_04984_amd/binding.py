@@ -24,8 +24,11 @@ EXPORTS = ("meft_workspace_bytes", "meft_check_shape", "meft_status_string", "me
            "meft_sparse_fwd", "meft_sparse_bwd", "meft_profile_enable", "meft_profile_read",
            "meft_probe_copy", "meft_probe_mfma", "meft_adam_rows", "meft_last_device_error",
            "meft_union_workspace_bytes", "meft_union_fwd", "meft_union_bwd", "meft_hostkv_stage",
-           "meft_debug_global_loads", "meft_route_static")
+           "meft_debug_global_loads", "meft_route_static", "meft_block_workspace_bytes", "meft_norm_fwd", "meft_norm_bwd",
+           "meft_dropout_add", "meft_add_norm_fwd", "meft_add_norm_bwd", "meft_route_scores", "meft_balance_fwd",
+           "meft_balance_bwd", "meft_route_bwd")
 MEFT_ROUTE_STATIC_BYTES = 16 << 20
+MEFT_NORM_LAYER, MEFT_NORM_RMS = 0, 1
 
 
 class MeftShape(ctypes.Structure):
@@ -38,6 +41,18 @@ class MeftShape(ctypes.Structure):
 class MeftAdam(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_float), ("beta1", ctypes.c_float), ("beta2", ctypes.c_float),
                 ("eps", ctypes.c_float), ("step", ctypes.c_int32)]
+
+
+class MeftNorm(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class MeftDrop(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_float), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64)]
+
+
+class MeftBalance(ctypes.Structure):
+    _fields_ = [("balance", ctypes.c_float), ("z", ctypes.c_float)]
 
 
 class MeftError(RuntimeError):
@@ -83,6 +98,16 @@ _lib.meft_union_bwd.restype = ctypes.c_int
 _lib.meft_union_bwd.argtypes = [_shape_p, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
 _lib.meft_hostkv_stage.restype = ctypes.c_int
 _lib.meft_hostkv_stage.argtypes = [_shape_p, _vp, _vp, _vp, _vp, _sz, _vp]
+_norm_p, _drop_p, _balance_p = (ctypes.POINTER(s) for s in (MeftNorm, MeftDrop, MeftBalance))
+_lib.meft_block_workspace_bytes.restype = _sz
+_lib.meft_block_workspace_bytes.argtypes = [_shape_p]
+for _name, _args in {"meft_norm_fwd": [_norm_p] + [_vp] * 6, "meft_norm_bwd": [_norm_p] + [_vp] * 10 + [_sz],
+                     "meft_dropout_add": [_drop_p] + [_vp] * 4, "meft_add_norm_fwd": [_norm_p, _drop_p] + [_vp] * 9,
+                     "meft_add_norm_bwd": [_norm_p, _drop_p] + [_vp] * 12 + [_sz], "meft_route_scores": [_vp] * 7 + [_sz],
+                     "meft_balance_fwd": [_balance_p] + [_vp] * 8 + [_sz], "meft_balance_bwd": [_balance_p] + [_vp] * 6,
+                     "meft_route_bwd": [_vp] * 8 + [_sz]}.items():
+    getattr(_lib, _name).restype = ctypes.c_int
+    getattr(_lib, _name).argtypes = [_shape_p] + _args + [_vp]
 _lib.meft_last_device_error.restype = ctypes.c_char_p
 _lib.meft_last_device_error.argtypes = []
 _lib.meft_probe_copy.restype = ctypes.c_int
@@ -213,6 +238,93 @@ def meft_adam_rows(shape, hp: MeftAdam, W, G, m, v, master, touched, n_touched, 
                              _p(m), _p(v), _p(master), _p(touched), _p(n_touched), _stream(stream))
     if check and rc:
         raise MeftError("meft_adam_rows", rc)
+    return rc
+
+
+def meft_block_workspace_bytes(shape: MeftShape) -> int:
+    return int(_lib.meft_block_workspace_bytes(ctypes.byref(shape)))
+
+
+def _ref(s):
+    return ctypes.byref(s) if s is not None else None
+
+
+def meft_norm_fwd(shape, norm: MeftNorm, x, gamma, beta, h, mean, rstd, stream=None, check=True) -> int:
+    rc = _lib.meft_norm_fwd(ctypes.byref(shape), _ref(norm), _p(x), _p(gamma), _p(beta), _p(h), _p(mean), _p(rstd),
+                            _stream(stream))
+    if check and rc:
+        raise MeftError("meft_norm_fwd", rc)
+    return rc
+
+
+def meft_norm_bwd(shape, norm: MeftNorm, x, gamma, mean, rstd, dh, dy, dx, dgamma, dbeta, ws, stream=None, check=True) -> int:
+    wp, wb = _ws(ws)
+    rc = _lib.meft_norm_bwd(ctypes.byref(shape), _ref(norm), _p(x), _p(gamma), _p(mean), _p(rstd), _p(dh), _p(dy), _p(dx),
+                            _p(dgamma), _p(dbeta), wp, wb, _stream(stream))
+    if check and rc:
+        raise MeftError("meft_norm_bwd", rc)
+    return rc
+
+
+def meft_dropout_add(shape, drop: Optional[MeftDrop], step, out, res, y, stream=None, check=True) -> int:
+    rc = _lib.meft_dropout_add(ctypes.byref(shape), _ref(drop), _p(step), _p(out), _p(res), _p(y), _stream(stream))
+    if check and rc:
+        raise MeftError("meft_dropout_add", rc)
+    return rc
+
+
+def meft_add_norm_fwd(shape, norm: MeftNorm, drop: Optional[MeftDrop], step, out, res, gamma, beta, y, h, mean, rstd,
+                      stream=None, check=True) -> int:
+    rc = _lib.meft_add_norm_fwd(ctypes.byref(shape), _ref(norm), _ref(drop), _p(step), _p(out), _p(res), _p(gamma), _p(beta),
+                                _p(y), _p(h), _p(mean), _p(rstd), _stream(stream))
+    if check and rc:
+        raise MeftError("meft_add_norm_fwd", rc)
+    return rc
+
+
+def meft_add_norm_bwd(shape, norm: MeftNorm, drop: Optional[MeftDrop], step, y, gamma, mean, rstd, dh, dy, dres, dout, dgamma,
+                      dbeta, ws, stream=None, check=True) -> int:
+    wp, wb = _ws(ws)
+    rc = _lib.meft_add_norm_bwd(ctypes.byref(shape), _ref(norm), _ref(drop), _p(step), _p(y), _p(gamma), _p(mean), _p(rstd),
+                                _p(dh), _p(dy), _p(dres), _p(dout), _p(dgamma), _p(dbeta), wp, wb, _stream(stream))
+    if check and rc:
+        raise MeftError("meft_add_norm_bwd", rc)
+    return rc
+
+
+def meft_route_scores(shape, h, Wg, bias, block_idx, block_score, scores, ws, stream=None, check=True) -> int:
+    wp, wb = _ws(ws)
+    rc = _lib.meft_route_scores(ctypes.byref(shape), _p(h), _p(Wg), _p(bias), _p(block_idx), _p(block_score), _p(scores), wp, wb,
+                                _stream(stream))
+    if check and rc:
+        raise MeftError("meft_route_scores", rc)
+    return rc
+
+
+def meft_balance_fwd(shape, balance: MeftBalance, scores, block_idx, valid, counts, n_valid, prob, loss, ws, stream=None,
+                     check=True) -> int:
+    wp, wb = _ws(ws)
+    rc = _lib.meft_balance_fwd(ctypes.byref(shape), _ref(balance), _p(scores), _p(block_idx), _p(valid), _p(counts), _p(n_valid),
+                               _p(prob), _p(loss), wp, wb, _stream(stream))
+    if check and rc:
+        raise MeftError("meft_balance_fwd", rc)
+    return rc
+
+
+def meft_balance_bwd(shape, balance: MeftBalance, scores, counts, n_valid, valid, dloss, dscores, stream=None, check=True) -> int:
+    rc = _lib.meft_balance_bwd(ctypes.byref(shape), _ref(balance), _p(scores), _p(counts), _p(n_valid), _p(valid), _p(dloss),
+                               _p(dscores), _stream(stream))
+    if check and rc:
+        raise MeftError("meft_balance_bwd", rc)
+    return rc
+
+
+def meft_route_bwd(shape, h, Wg, dscores, add, dh, dWg, dbias, ws, stream=None, check=True) -> int:
+    wp, wb = _ws(ws)
+    rc = _lib.meft_route_bwd(ctypes.byref(shape), _p(h), _p(Wg), _p(dscores), _p(add), _p(dh), _p(dWg), _p(dbias), wp, wb,
+                             _stream(stream))
+    if check and rc:
+        raise MeftError("meft_route_bwd", rc)
     return rc
 
 

@@ -8,24 +8,38 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmeft.so")
-SOURCES = [os.path.join(CSRC, "meft_api.hip")]
-FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-shared", "-fPIC",
+# the first one's kernels come first in the library
+SOURCES = [os.path.join(CSRC, n) for n in ("meft_api.hip", "block_api.hip")]
+FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function"]
 
 
-def build_library(verbose: bool = True) -> str:
-    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc, *FLAGS, "-o", LIB, *SOURCES]
+def _start(cmd, verbose):
     if verbose:
         print(" ".join(cmd), flush=True)
-    proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    # the host pass does not know the packed-fp32 target feature and says so once per file: harmless
-    out = "\n".join(l for l in proc.stdout.splitlines() if "packed-fp32-ops" not in l)
-    if out.strip() and (verbose or proc.returncode):
-        print(out, flush=True)
-    if proc.returncode:
+    return subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+
+
+def _finish(procs, verbose):
+    failed = False
+    for proc in procs:
+        text, _ = proc.communicate()
+        # the host pass does not know the packed-fp32 target feature and says so once per file: harmless
+        out = "\n".join(l for l in text.splitlines() if "packed-fp32-ops" not in l)
+        if out.strip() and (verbose or proc.returncode):
+            print(out, flush=True)
+        failed |= proc.returncode != 0
+    if failed:
         raise RuntimeError("hipcc failed")
+
+
+def build_library(verbose: bool = True, sources=None) -> str:
+    """Compiles the sources side by side and links them.  `sources`: only these anew, the others' objects as they are."""
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    objects = {s: os.path.splitext(s)[0] + ".o" for s in SOURCES}
+    _finish([_start([hipcc, *FLAGS, "-c", "-o", objects[s], s], verbose) for s in sources or SOURCES], verbose)
+    _finish([_start([hipcc, *FLAGS, "-shared", "-o", LIB, *objects.values()], verbose)], verbose)
     return LIB
 
 

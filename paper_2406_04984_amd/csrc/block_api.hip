@@ -1,0 +1,438 @@
+// Host side of the calls around the layer (include/meft.h): norms, dropout, the router's balance loss and its gradient.
+// Argument validation, workspace layout and launches; the kernels are in the headers included below.
+#include <cmath>
+#include <mutex>
+
+#include "balance.h"
+#include "dropout.h"
+#include "host.h"
+#include "norm.h"
+#include "router_grad.h"
+
+namespace meft {
+namespace {
+
+constexpr int kCus = 256;   // compute units of an MI355X
+
+template <typename T>
+bool aligned_as(const void* p) { return reinterpret_cast<uintptr_t>(p) % alignof(T) == 0; }
+bool ok16(const void* p) { return p && aligned16(p); }
+bool null_or16(const void* p) { return !p || aligned16(p); }
+
+// ---- norms ----------------------------------------------------------------------------------
+// Waves per row and groups of eight columns per lane.
+struct NormShape {
+  int v, w;
+};
+NormShape norm_shape(int d) {
+  const int groups = d / 8;
+  if (groups <= 64) return {1, 1};
+  if (groups <= 128) return {2, 1};
+  if (groups <= 256) return {1, 4};
+  if (groups <= 512) return {2, 4};
+  if (groups <= 1024) return {2, 8};
+  return {2, 16};
+}
+
+constexpr int kNormBwdWgs = 512;
+int norm_bwd_slots(int w) { return w > 8 ? 1 : 8 / w; }
+// workgroups of the backward, each of which leaves partial sums of dgamma and dbeta
+int norm_bwd_grid(const meft_shape& s) {
+  const int slots = norm_bwd_slots(norm_shape(s.d).w);
+  const int64_t need = ((int64_t)s.T + slots - 1) / slots;
+  return (int)(need < 1 ? 1 : need < kNormBwdWgs ? need : kNormBwdWgs);
+}
+
+#define MEFT_NORM_SHAPES(X) X(1, 1) X(2, 1) X(1, 4) X(2, 4) X(2, 8) X(2, 16)
+
+template <typename T, int kMode>
+void launch_norm_fwd(const meft_shape& s, const NormFwdArgs<T>& a, hipStream_t st) {
+  const NormShape n = norm_shape(s.d);
+  const int slots = n.w > 4 ? 1 : 4 / n.w, threads = n.w > 4 ? 64 * n.w : 256;
+  const int64_t need = ((int64_t)s.T + slots - 1) / slots, most = (int64_t)kCus * (2048 / threads);
+  const dim3 grid((unsigned)(need < most ? need : most));
+#define X(V, W) \
+  if (n.v == V && n.w == W) MEFT_LAUNCH("norm_fwd", (norm_fwd_kernel<T, V, W, kMode>), grid, dim3(threads), 0, st, a);
+  MEFT_NORM_SHAPES(X)
+#undef X
+}
+
+template <typename T, int kMode, int kGrads>
+void launch_norm_bwd(const meft_shape& s, const NormBwdArgs<T>& a, hipStream_t st) {
+  const NormShape n = norm_shape(s.d);
+  const dim3 grid(norm_bwd_grid(s)), block(n.w > 8 ? 64 * n.w : 512);
+#define X(V, W) \
+  if (n.v == V && n.w == W) MEFT_LAUNCH("norm_bwd", (norm_bwd_kernel<T, V, W, kMode, kGrads>), grid, block, 0, st, a);
+  MEFT_NORM_SHAPES(X)
+#undef X
+}
+
+bool norm_ok(const meft_norm* n) {
+  return n && (n->kind == MEFT_NORM_LAYER || n->kind == MEFT_NORM_RMS) && n->eps >= 0.f && std::isfinite(n->eps);
+}
+
+// 0 where nothing is dropped; -1: not a valid share
+int drop_threshold(const meft_drop* d) {
+  if (!d) return 0;
+  if (!(d->p >= 0.f && d->p < 1.f)) return -1;
+  const int thr = (int)std::floor((double)d->p * 65536.0 + 0.5);
+  return thr <= 65535 ? thr : -1;
+}
+
+DropArgs drop_args(const meft_drop* d, const uint64_t* step, int thr) {
+  DropArgs a{};
+  if (d) {
+    a.k0 = (uint32_t)d->seed;
+    a.k1 = (uint32_t)(d->seed >> 32);
+    a.offset = d->offset;
+  }
+  a.step = step;
+  a.thr = (uint32_t)thr;
+  a.scale = (float)(65536.0 / (65536.0 - thr));
+  return a;
+}
+
+template <typename T>
+meft_status norm_fwd(const meft_shape& s, const meft_norm& n, int mode, const DropArgs& drop, const void* x, const void* out,
+                     const void* gamma, const void* beta, void* y, void* h, float* mean, float* rstd, hipStream_t st) {
+  const NormFwdArgs<T> a{static_cast<const T*>(x), static_cast<const T*>(out), static_cast<const T*>(gamma), static_cast<const T*>(beta),
+                         static_cast<T*>(y), static_cast<T*>(h), mean, rstd, s.T, s.d, n.kind == MEFT_NORM_LAYER,
+                         (float)(1.0 / s.d), n.eps, drop};
+  if (mode == kNormPlain) launch_norm_fwd<T, kNormPlain>(s, a, st);
+  else if (mode == kNormAdd) launch_norm_fwd<T, kNormAdd>(s, a, st);
+  else launch_norm_fwd<T, kNormDrop>(s, a, st);
+  return launch_status();
+}
+
+struct NormBwdWs {
+  float* part;
+  size_t bytes;
+  NormBwdWs(const meft_shape& s, void* ws) {
+    Carver c(ws);
+    part = c.take<float>((size_t)norm_bwd_grid(s) * 2 * s.d);
+    bytes = c.off;
+  }
+};
+
+template <typename T, int kMode>
+void norm_bwd_grads(const meft_shape& s, const NormBwdArgs<T>& a, int grads, hipStream_t st) {
+  if (grads == 0) launch_norm_bwd<T, kMode, 0>(s, a, st);
+  else if (grads == 1) launch_norm_bwd<T, kMode, 1>(s, a, st);
+  else launch_norm_bwd<T, kMode, 2>(s, a, st);
+}
+
+template <typename T>
+meft_status norm_bwd(const meft_shape& s, const meft_norm& n, int mode, const DropArgs& drop, const void* y, const void* gamma,
+                     const float* mean, const float* rstd, const void* dh, const void* dy, void* dx, void* dout, void* dgamma,
+                     void* dbeta, void* ws, hipStream_t st) {
+  const NormBwdWs w(s, ws);
+  const int grads = !dgamma ? 0 : dbeta ? 2 : 1;
+  if (s.T == 0 && grads == 0) return MEFT_OK;
+  const NormBwdArgs<T> a{static_cast<const T*>(y), static_cast<const T*>(gamma), static_cast<const T*>(dh), static_cast<const T*>(dy),
+                         mean, rstd, static_cast<T*>(dx), static_cast<T*>(dout), w.part, s.T, s.d, n.kind == MEFT_NORM_LAYER,
+                         (float)(1.0 / s.d), drop};
+  if (mode == kNormPlain) norm_bwd_grads<T, kNormPlain>(s, a, grads, st);
+  else if (mode == kNormAdd) norm_bwd_grads<T, kNormAdd>(s, a, grads, st);
+  else norm_bwd_grads<T, kNormDrop>(s, a, grads, st);
+  if (grads)
+    MEFT_LAUNCH("norm_grad", norm_grad_kernel<T>, dim3((s.d + 63) / 64, grads), dim3(256), 0, st, w.part, norm_bwd_grid(s), s.d,
+                static_cast<T*>(dgamma), static_cast<T*>(dbeta));
+  return launch_status();
+}
+
+// ---- balance --------------------------------------------------------------------------------
+// waves of a row of scores
+int balance_waves(const meft_shape& s) { return s.n_blocks <= 1024 ? 1 : 16; }
+int balance_grid(const meft_shape& s) {
+  const int rows = balance_waves(s) == 1 ? 4 : 1;
+  const int64_t need = ((int64_t)s.T + rows - 1) / rows;
+  return (int)(need < 1 ? 1 : need < kCus ? need : kCus);
+}
+
+struct BalanceWs : BalancePart {
+  size_t bytes;
+  BalanceWs(const meft_shape& s, void* ws) {
+    Carver c(ws);
+    const size_t g = balance_grid(s);
+    prob = c.take<float>(g * s.n_blocks);
+    count = c.take<int32_t>(g * s.n_blocks);
+    lse2 = c.take<float>(g);
+    tokens = c.take<int32_t>(g);
+    dot = c.take<float>((s.n_blocks + 63) / 64);
+    ticket = c.take<uint32_t>(1);
+    bytes = c.off;
+  }
+};
+
+#define MEFT_BALANCE_SHAPES(X)                                                     \
+  if (s.n_blocks <= 64) X(1, 1);                                                   \
+  else if (s.n_blocks <= 128) X(2, 1);                                             \
+  else if (s.n_blocks <= 256) X(4, 1);                                             \
+  else if (s.n_blocks <= 512) X(8, 1);                                             \
+  else if (s.n_blocks <= 1024) X(16, 1);                                           \
+  else if (s.n_blocks <= 2048) X(2, 16);                                           \
+  else if (s.n_blocks <= 4096) X(4, 16);                                           \
+  else if (s.n_blocks <= 8192) X(8, 16);                                           \
+  else X(16, 16)
+static_assert(kMaxBlocks <= 16 * 16 * 64, "balance_part_kernel and balance_grad_kernel hold a row in registers");
+
+template <int Z, int W>
+void launch_balance_part(const meft_shape& s, const float* scores, const int32_t* block_idx, const uint8_t* valid,
+                         const BalancePart& part, hipStream_t st) {
+  const size_t lds = (size_t)s.n_blocks * 4 * (W == 1 ? 5 : 1);
+  if (W > 1) {
+    static std::once_flag configured;   // up to 64 KB of counts beside the waves' values
+    std::call_once(configured, [] {
+      (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&balance_part_kernel<Z, W>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                kMaxBlocks * 4);
+    });
+  }
+  MEFT_LAUNCH("balance_part", (balance_part_kernel<Z, W>), dim3(balance_grid(s)), dim3(W == 1 ? 256 : 64 * W), lds, st, scores,
+              block_idx, valid, s.T, s.n_blocks, s.top_e, part);
+}
+
+bool balance_ok(const meft_balance* b) { return b && std::isfinite(b->balance) && std::isfinite(b->z); }
+
+// ---- router gradient ------------------------------------------------------------------------
+struct RouteGradPlan {
+  int slices, m, m_waves, groups, splits, per_split;
+};
+RouteGradPlan route_grad_plan(const meft_shape& s) {
+  RouteGradPlan p{};
+  p.slices = (s.d + kRgCols - 1) / kRgCols;
+  p.m = s.n_blocks <= 32 ? 1 : 2;
+  const int tiles = (s.n_blocks + 32 * p.m - 1) / (32 * p.m);
+  p.m_waves = tiles >= 3 ? 4 : tiles;
+  p.groups = (tiles + p.m_waves - 1) / p.m_waves;
+  // as many splits of the tokens as give every compute unit a workgroup, each at least four steps of 16 tokens per wave
+  const int64_t least = 16 * (4 / p.m_waves) * 4, want = (kCus + p.slices * p.groups - 1) / (p.slices * p.groups);
+  const int64_t can = (s.T + least - 1) / least;
+  int64_t splits = want < can ? want : can;
+  if (splits < 1) splits = 1;
+  const int64_t per = ((s.T + splits - 1) / splits + 15) / 16 * 16;
+  p.per_split = (int)(per < 16 ? 16 : per);
+  splits = ((int64_t)s.T + p.per_split - 1) / p.per_split;
+  p.splits = (int)(splits < 1 ? 1 : splits);
+  return p;
+}
+
+struct RouteGradWs {
+  float *part, *part_bias;
+  size_t bytes;
+  RouteGradWs(const meft_shape& s, void* ws) {
+    Carver c(ws);
+    const RouteGradPlan p = route_grad_plan(s);
+    part = c.take<float>(p.splits > 1 ? (size_t)p.splits * s.n_blocks * s.d : 0);
+    part_bias = c.take<float>(p.splits > 1 ? (size_t)p.splits * s.n_blocks : 0);
+    bytes = c.off;
+  }
+};
+
+template <typename T>
+meft_status route_bwd(const meft_shape& s, const void* h, const void* Wg, const float* ds, const void* add, void* dh, void* dWg,
+                      float* dbias, void* ws, hipStream_t st) {
+  const RouteGradPlan p = route_grad_plan(s);
+  const RouteGradWs w(s, ws);
+  const RouteGradArgs<T> a{static_cast<const T*>(h), static_cast<const T*>(Wg), static_cast<const T*>(add), ds, static_cast<T*>(dh),
+                           static_cast<T*>(dWg), dbias, w.part, w.part_bias, s.T, s.d, s.n_blocks, p.slices, p.m_waves, p.splits,
+                           p.per_split};
+  if (dh && s.T > 0) {
+    const int64_t tiles = ((int64_t)s.T + 4 * kRgTok - 1) / (4 * kRgTok);
+    MEFT_LAUNCH("route_dh", route_dh_kernel<T>, dim3((unsigned)(tiles * p.slices)), dim3(256), 0, st, a);
+  }
+  if (dWg || dbias) {
+    const dim3 grid(dWg ? p.slices : 1, p.groups, p.splits);
+    if (p.m == 1) MEFT_LAUNCH("route_dw", (route_dw_kernel<T, 1>), grid, dim3(256), 0, st, a);
+    else MEFT_LAUNCH("route_dw", (route_dw_kernel<T, 2>), grid, dim3(256), 0, st, a);
+    if (p.splits > 1) {
+      const int64_t quads = dWg ? (int64_t)s.n_blocks * s.d / 4 : 0;
+      MEFT_LAUNCH("route_dw_join", route_dw_join_kernel<T>, dim3((unsigned)((quads + 255) / 256 + 1)), dim3(256), 0, st, a);
+    }
+  }
+  return launch_status();
+}
+
+size_t block_workspace_bytes(const meft_shape& s) {
+  size_t m = 256;
+  for (const size_t b : {NormBwdWs(s, nullptr).bytes, BalanceWs(s, nullptr).bytes, RouteGradWs(s, nullptr).bytes})
+    if (b > m) m = b;
+  return m;
+}
+
+meft_status check_block_ws(const meft_shape& s, const void* ws, size_t have) {
+  if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u) || have < block_workspace_bytes(s)) return MEFT_ERR_WORKSPACE;
+  return MEFT_OK;
+}
+
+}  // namespace
+}  // namespace meft
+
+using namespace meft;
+
+#define MEFT_BY_TYPE(f, ...) (s.dtype == MEFT_BF16 ? f<bf16_t>(__VA_ARGS__) : f<float>(__VA_ARGS__))
+
+extern "C" {
+
+size_t meft_block_workspace_bytes(const meft_shape* shape) {
+  if (check_shape(shape) != MEFT_OK) return 0;
+  return block_workspace_bytes(*shape);
+}
+
+meft_status meft_norm_fwd(const meft_shape* shape, const meft_norm* norm, const void* x, const void* gamma, const void* beta,
+                          void* h, float* mean, float* rstd, void* stream) {
+  const meft_status rc = check_shape(shape);
+  if (rc != MEFT_OK) return rc;
+  const meft_shape& s = *shape;
+  if (!norm_ok(norm) || !ok16(x) || !ok16(gamma) || !null_or16(beta) || !ok16(h) || !aligned_as<float>(mean) || !aligned_as<float>(rstd))
+    return MEFT_ERR_INVALID_ARG;
+  if (s.T == 0) return MEFT_OK;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  MEFT_API_LOCK();
+  clear_stale_error();
+  return MEFT_BY_TYPE(norm_fwd, s, *norm, kNormPlain, DropArgs{}, x, nullptr, gamma, beta, nullptr, h, mean, rstd, st);
+}
+
+meft_status meft_norm_bwd(const meft_shape* shape, const meft_norm* norm, const void* x, const void* gamma, const float* mean,
+                          const float* rstd, const void* dh, const void* dy, void* dx, void* dgamma, void* dbeta, void* ws,
+                          size_t ws_bytes, void* stream) {
+  meft_status rc = check_shape(shape);
+  if (rc != MEFT_OK) return rc;
+  const meft_shape& s = *shape;
+  if (!norm_ok(norm) || !ok16(x) || !ok16(gamma) || !rstd || !aligned_as<float>(rstd) || !ok16(dh) || !null_or16(dy) || !ok16(dx) ||
+      !null_or16(dgamma) || !null_or16(dbeta) || (dbeta && !dgamma))
+    return MEFT_ERR_INVALID_ARG;
+  if (!aligned_as<float>(mean) || (norm->kind == MEFT_NORM_LAYER && !mean)) return MEFT_ERR_INVALID_ARG;
+  if ((rc = check_block_ws(s, ws, ws_bytes)) != MEFT_OK) return rc;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  MEFT_API_LOCK();
+  clear_stale_error();
+  return MEFT_BY_TYPE(norm_bwd, s, *norm, kNormPlain, DropArgs{}, x, gamma, mean, rstd, dh, dy, dx, nullptr, dgamma, dbeta, ws, st);
+}
+
+meft_status meft_dropout_add(const meft_shape* shape, const meft_drop* drop, const uint64_t* step, const void* out, const void* res,
+                             void* y, void* stream) {
+  const meft_status rc = check_shape(shape);
+  if (rc != MEFT_OK) return rc;
+  const meft_shape& s = *shape;
+  const int thr = drop_threshold(drop);
+  if (thr < 0 || !aligned_as<uint64_t>(step) || !ok16(out) || !null_or16(res) || !ok16(y)) return MEFT_ERR_INVALID_ARG;
+  if (s.T == 0) return MEFT_OK;
+  const int groups = s.d / 8;
+  const int64_t wgs = ((int64_t)s.T * groups + 256 * kDropGroups - 1) / (256 * kDropGroups), x = wgs < (1 << 23) ? wgs : 1 << 23;
+  const dim3 grid((unsigned)x, (unsigned)((wgs + x - 1) / x));   // a launch takes fewer than 2^32 threads along x
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const DropArgs a = drop_args(drop, step, thr);
+  MEFT_API_LOCK();
+  clear_stale_error();
+#define DROPOUT(TY, DROP) MEFT_LAUNCH("dropout_add", (dropout_add_kernel<TY, DROP>), grid, dim3(256), 0, st, static_cast<const TY*>(out), \
+                                     static_cast<const TY*>(res), static_cast<TY*>(y), s.T, groups, tile_div_inverse(groups), a)
+  if (s.dtype == MEFT_BF16) {
+    if (thr) DROPOUT(bf16_t, true);
+    else DROPOUT(bf16_t, false);
+  } else {
+    if (thr) DROPOUT(float, true);
+    else DROPOUT(float, false);
+  }
+#undef DROPOUT
+  return launch_status();
+}
+
+meft_status meft_add_norm_fwd(const meft_shape* shape, const meft_norm* norm, const meft_drop* drop, const uint64_t* step,
+                              const void* out, const void* res, const void* gamma, const void* beta, void* y, void* h, float* mean,
+                              float* rstd, void* stream) {
+  const meft_status rc = check_shape(shape);
+  if (rc != MEFT_OK) return rc;
+  const meft_shape& s = *shape;
+  const int thr = drop_threshold(drop);
+  if (!norm_ok(norm) || thr < 0 || !aligned_as<uint64_t>(step) || !ok16(out) || !ok16(res) || !ok16(gamma) || !null_or16(beta) ||
+      !ok16(y) || !ok16(h) || y == h || !aligned_as<float>(mean) || !aligned_as<float>(rstd))
+    return MEFT_ERR_INVALID_ARG;
+  if (s.T == 0) return MEFT_OK;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  MEFT_API_LOCK();
+  clear_stale_error();
+  return MEFT_BY_TYPE(norm_fwd, s, *norm, thr ? kNormDrop : kNormAdd, drop_args(drop, step, thr), res, out, gamma, beta, y, h, mean,
+                      rstd, st);
+}
+
+meft_status meft_add_norm_bwd(const meft_shape* shape, const meft_norm* norm, const meft_drop* drop, const uint64_t* step,
+                              const void* y, const void* gamma, const float* mean, const float* rstd, const void* dh, const void* dy,
+                              void* dres, void* dout, void* dgamma, void* dbeta, void* ws, size_t ws_bytes, void* stream) {
+  meft_status rc = check_shape(shape);
+  if (rc != MEFT_OK) return rc;
+  const meft_shape& s = *shape;
+  const int thr = drop_threshold(drop);
+  if (!norm_ok(norm) || thr < 0 || !aligned_as<uint64_t>(step) || !ok16(y) || !ok16(gamma) || !rstd || !aligned_as<float>(rstd) ||
+      !ok16(dh) || !null_or16(dy) || !ok16(dres) || !ok16(dout) || dres == dout || !null_or16(dgamma) || !null_or16(dbeta) ||
+      (dbeta && !dgamma))
+    return MEFT_ERR_INVALID_ARG;
+  if (!aligned_as<float>(mean) || (norm->kind == MEFT_NORM_LAYER && !mean)) return MEFT_ERR_INVALID_ARG;
+  if ((rc = check_block_ws(s, ws, ws_bytes)) != MEFT_OK) return rc;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  MEFT_API_LOCK();
+  clear_stale_error();
+  return MEFT_BY_TYPE(norm_bwd, s, *norm, thr ? kNormDrop : kNormAdd, drop_args(drop, step, thr), y, gamma, mean, rstd, dh, dy, dres,
+                      dout, dgamma, dbeta, ws, st);
+}
+
+meft_status meft_balance_fwd(const meft_shape* shape, const meft_balance* balance, const float* scores, const int32_t* block_idx,
+                             const uint8_t* valid, int32_t* counts, int32_t* n_valid, float* prob, float* loss, void* ws,
+                             size_t ws_bytes, void* stream) {
+  meft_status rc = check_shape(shape);
+  if (rc != MEFT_OK) return rc;
+  const meft_shape& s = *shape;
+  if (!balance_ok(balance) || !ok16(scores) || !block_idx || !counts || !n_valid || !prob || !loss || !aligned_as<int32_t>(block_idx) ||
+      !aligned_as<int32_t>(counts) || !aligned_as<int32_t>(n_valid) || !aligned_as<float>(prob) || !aligned_as<float>(loss))
+    return MEFT_ERR_INVALID_ARG;
+  if ((rc = check_block_ws(s, ws, ws_bytes)) != MEFT_OK) return rc;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const BalanceWs w(s, ws);
+  MEFT_API_LOCK();
+  clear_stale_error();
+#define X(Z, W) launch_balance_part<Z, W>(s, scores, block_idx, valid, w, st)
+  MEFT_BALANCE_SHAPES(X);
+#undef X
+  MEFT_LAUNCH("balance_join", balance_join_kernel, dim3((s.n_blocks + 63) / 64), dim3(1024), 0, st, static_cast<const BalancePart&>(w),
+              balance_grid(s), s.n_blocks, s.top_e, balance->balance, balance->z, counts, n_valid, prob, loss);
+  return launch_status();
+}
+
+meft_status meft_balance_bwd(const meft_shape* shape, const meft_balance* balance, const float* scores, const int32_t* counts,
+                             const int32_t* n_valid, const uint8_t* valid, const float* dloss, float* dscores, void* stream) {
+  const meft_status rc = check_shape(shape);
+  if (rc != MEFT_OK) return rc;
+  const meft_shape& s = *shape;
+  if (!balance_ok(balance) || !ok16(scores) || !counts || !n_valid || !ok16(dscores) || !aligned_as<int32_t>(counts) ||
+      !aligned_as<int32_t>(n_valid) || !aligned_as<float>(dloss))
+    return MEFT_ERR_INVALID_ARG;
+  if (s.T == 0) return MEFT_OK;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const int rows = balance_waves(s) == 1 ? 4 : 1;
+  const int64_t need = ((int64_t)s.T + rows - 1) / rows, most = kCus * 8;
+  const dim3 grid((unsigned)(need < most ? need : most));
+  MEFT_API_LOCK();
+  clear_stale_error();
+#define X(Z, W)                                                                                                             \
+  MEFT_LAUNCH("balance_grad", (balance_grad_kernel<Z, W>), grid, dim3(W == 1 ? 256 : 64 * W), 0, st, scores, counts, n_valid, valid, \
+              dloss, s.T, s.n_blocks, s.top_e, balance->balance, balance->z, dscores)
+  MEFT_BALANCE_SHAPES(X);
+#undef X
+  return launch_status();
+}
+
+meft_status meft_route_bwd(const meft_shape* shape, const void* h, const void* Wg, const float* dscores, const void* add, void* dh,
+                           void* dWg, float* dbias, void* ws, size_t ws_bytes, void* stream) {
+  meft_status rc = check_shape(shape);
+  if (rc != MEFT_OK) return rc;
+  const meft_shape& s = *shape;
+  if (!ok16(h) || !ok16(Wg) || !ok16(dscores) || !null_or16(add) || !null_or16(dh) || !null_or16(dWg) || !aligned_as<float>(dbias) ||
+      !(dh || dWg || dbias) || (add && !dh))
+    return MEFT_ERR_INVALID_ARG;
+  if ((rc = check_block_ws(s, ws, ws_bytes)) != MEFT_OK) return rc;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  MEFT_API_LOCK();
+  clear_stale_error();
+  return MEFT_BY_TYPE(route_bwd, s, h, Wg, dscores, add, dh, dWg, dbias, ws, st);
+}
+
+}  // extern "C"

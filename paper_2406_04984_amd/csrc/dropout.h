@@ -1,0 +1,81 @@
+// Dropout whose mask is a function of the element's place: y = res + keep(t, c) * out * scale, forward and backward alike.
+//
+// The mask is that of Philox4x32 with 10 rounds (Salmon et al., "Parallel random numbers: as easy as 1, 2, 3", 2011): the
+// counter of columns 8 g .. 8 g + 7 of token t is (g, t, low word, high word of the offset), the key the seed.  Each of the
+// four result words serves two columns with 16 bits each, the low ones first: an element is kept where its 16 bits are at
+// least thr.  16 bits make the dropped share a multiple of 2^-16 (scale = 65536 / (65536 - thr) is the exact inverse of the
+// kept one, so the expectation is that of `out`) and cost half the generator's multiplications of 32.
+#pragma once
+#include "common.h"
+#include "tile_div.h"
+
+namespace meft {
+
+struct DropArgs {
+  uint32_t k0, k1;               // seed
+  uint64_t offset;
+  const uint64_t* step;          // added to the offset where given: a captured launch draws anew in every replay
+  uint32_t thr;                  // dropped where the 16 bits are below; 0: nothing is dropped
+  float scale;
+};
+
+__device__ __forceinline__ uint64_t drop_offset(const DropArgs& a) { return a.offset + (a.step ? *a.step : 0ull); }
+
+__device__ __forceinline__ u32x4 philox4x32(u32x4 c, uint32_t k0, uint32_t k1) {
+#pragma unroll
+  for (int r = 0; r < 10; ++r) {
+    const uint64_t a = (uint64_t)c.x * 0xD2511F53u, b = (uint64_t)c.z * 0xCD9E8D57u;
+    c = u32x4{(uint32_t)(b >> 32) ^ c.y ^ k0, (uint32_t)b, (uint32_t)(a >> 32) ^ c.w ^ k1, (uint32_t)a};
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  return c;
+}
+
+// v[j] = kept ? v[j] * scale : 0 for the eight columns of group g of token t
+__device__ __forceinline__ void drop8(const DropArgs& a, uint64_t offset, uint32_t t, uint32_t g, float (&v)[8]) {
+  const u32x4 w = philox4x32(u32x4{g, t, (uint32_t)offset, (uint32_t)(offset >> 32)}, a.k0, a.k1);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = (w[i] & 0xFFFFu) >= a.thr ? v[2 * i] * a.scale : 0.f;
+    v[2 * i + 1] = (w[i] >> 16) >= a.thr ? v[2 * i + 1] * a.scale : 0.f;
+  }
+}
+
+constexpr int kDropGroups = 4;   // groups of eight columns per thread
+
+// One workgroup takes 256 * kDropGroups consecutive groups.  y may be out or res: a thread reads its elements before it
+// writes them.
+template <typename T, bool kDrop>
+__global__ __launch_bounds__(256) void dropout_add_kernel(const T* out, const T* res, T* y, int n_tok, int groups, uint32_t inv,
+                                                          DropArgs a) {
+  constexpr int kSpan = 256 * kDropGroups;
+  const uint64_t total = (uint64_t)n_tok * groups, first = ((uint64_t)blockIdx.y * gridDim.x + blockIdx.x) * kSpan;
+  if (first >= total) return;
+  const uint32_t t0 = (uint32_t)(first / (uint32_t)groups), g0 = (uint32_t)(first % (uint32_t)groups);
+  const uint64_t offset = kDrop ? drop_offset(a) : 0;
+  float v[kDropGroups][8], r[kDropGroups][8];
+#pragma unroll
+  for (int u = 0; u < kDropGroups; ++u) {
+    const uint64_t i = first + u * 256 + threadIdx.x;
+    if (i >= total) continue;
+    Vec8<T>::load(out + i * 8, v[u]);
+    if (res) Vec8<T>::load(res + i * 8, r[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < kDropGroups; ++u) {
+    const uint64_t i = first + u * 256 + threadIdx.x;
+    if (i >= total) continue;
+    if (kDrop) {
+      const uint32_t w = g0 + u * 256 + threadIdx.x, dt = (uint32_t)tile_div((int)w, groups, inv);
+      drop8(a, offset, t0 + dt, w - dt * groups, v[u]);
+    }
+    if (res) {
+#pragma unroll
+      for (int z = 0; z < 8; ++z) v[u][z] += r[u][z];
+    }
+    Vec8<T>::store(y + i * 8, v[u]);
+  }
+}
+
+}  // namespace meft

@@ -7,7 +7,6 @@
 #include <cstdint>
 #include <cstdlib>
 #include <cstring>
-#include <mutex>
 #include <string>
 #include <vector>
 
@@ -19,6 +18,7 @@
 #include "few_tokens.h"
 #include "gather.h"
 #include "gemm_nt.h"
+#include "host.h"
 #include "router.h"
 #include "scatter.h"
 #include "select.h"
@@ -30,56 +30,22 @@
 static __device__ __align__(256) unsigned char scratch[MEFT_ROUTE_STATIC_BYTES];
 
 namespace meft {
-namespace {
 
-// The host side of every entry point that enqueues work or touches the library's few pieces of process-wide state
-// (the timing list, the side stream and events of the host-resident variant, the table of staged workspaces) runs
-// under this lock, so the entry points may be called from several host threads.
 std::mutex g_api_mutex;
-#define MEFT_API_LOCK() std::lock_guard<std::mutex> api_lock_(g_api_mutex)
-
-// ---- per-kernel timing ----------------------------------------------------------------------
-struct ProfEntry {
-  const char* name;
-  hipEvent_t start, stop;
-};
 bool g_prof_on = false;
 std::vector<ProfEntry> g_prof;
 
-struct LaunchScope {
-  hipStream_t st;
-  bool on;
-  hipEvent_t stop{};
-  LaunchScope(const char* name, hipStream_t s) : st(s), on(g_prof_on) {
-    if (!on) return;
-    ProfEntry e{name, nullptr, nullptr};
-    if (hipEventCreate(&e.start) != hipSuccess || hipEventCreate(&e.stop) != hipSuccess) {
-      on = false;
-      return;
-    }
-    (void)hipEventRecord(e.start, st);
-    stop = e.stop;
-    g_prof.push_back(e);
-  }
-  ~LaunchScope() {
-    if (on) (void)hipEventRecord(stop, st);
-  }
-};
-
-#define MEFT_LAUNCH(name, kernel, grid, block, shmem, stream, ...)            \
-  do {                                                                        \
-    LaunchScope scope_(name, stream);                                         \
-    hipLaunchKernelGGL(kernel, grid, block, shmem, stream, __VA_ARGS__);      \
-  } while (0)
+namespace {
 
 // ---- shape checks ---------------------------------------------------------------------------
-constexpr int kMaxD = 16384, kMaxBlocks = 16384;
 constexpr int kMaxC = 1 << 22;      // candidates per token (top_e * block_size)
 // few out of more candidates than this: topk_select_bound_kernel, whose 1024 threads need four each.  Forward without the
 // value sum, 2048 tokens, registers / bound: 16 of 4160 75 / 60 us, 64 of 4160 78 / 68, 256 of 4160 85 / 82, 256 of 12288
 // 168 / 142.
 constexpr int kBoundMinC = 4096;
 constexpr int kMaxLdsC = 12288;     // up to here the top-k selection keeps a token's keys in LDS
+
+}  // namespace
 
 meft_status check_shape(const meft_shape* s) {
   if (!s) return MEFT_ERR_INVALID_ARG;
@@ -99,21 +65,9 @@ meft_status check_shape(const meft_shape* s) {
   return MEFT_OK;
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+namespace {
 
 // ---- workspace layout -----------------------------------------------------------------------
-struct Carver {
-  char* base;
-  size_t off = 0;
-  explicit Carver(void* b) : base(static_cast<char*>(b)) {}
-  template <typename T>
-  T* take(size_t n) {
-    T* p = base ? reinterpret_cast<T*>(base + off) : nullptr;
-    off += (n * sizeof(T) + 255) & ~(size_t)255;
-    return p;
-  }
-};
-
 // The matrix-core formulation (dense_path.h) is used for bf16 when the hidden size fits its k tiling and
 // the selection is dense enough inside the chosen blocks; otherwise, and for fp32, the per-pair gather
 // kernels are used.
@@ -495,15 +449,17 @@ meft_status check_ws(const meft_shape& s, const void* ws, size_t have) {
 }
 
 thread_local hipError_t g_last_device_error = hipSuccess;   // what the last MEFT_ERR_DEVICE of this thread was
+
+}  // namespace
+
 meft_status launch_status() {
   const hipError_t e = hipGetLastError();
   if (e == hipSuccess) return MEFT_OK;
   g_last_device_error = e;
   return MEFT_ERR_DEVICE;
 }
-// The runtime keeps the last error of the thread until it is read: an entry point reads it away before its first
-// launch, so that MEFT_ERR_DEVICE reports this call's own launches and not a failure some other code left behind.
-void clear_stale_error() { (void)hipGetLastError(); }
+
+namespace {
 
 // threads per workgroup and 8-column groups per thread for the row kernels
 void row_launch(int d, int& nthr, int& nv) {
@@ -1090,9 +1046,9 @@ static int launch_route_part(const meft_shape& s, const void* h, const void* Wg,
 }
 
 // Router scores (as up to kRouterSplitMax partial sums over slices of the hidden dimension, in `p`) and the top-e
-// selection over their sum.
+// selection over their sum.  scores: null, or where the sums go.
 static meft_status route_impl(const meft_shape& s, const void* h, const void* Wg, const float* bias,
-                              int32_t* block_idx, float* block_score, float* p, hipStream_t st) {
+                              int32_t* block_idx, float* block_score, float* scores, float* p, hipStream_t st) {
   int n_part = 1;
   if (!route_on_tiles(s)) {
     n_part = s.dtype == MEFT_BF16 ? launch_route_part<bf16_t>(s, h, Wg, p, st) : launch_route_part<float>(s, h, Wg, p, st);
@@ -1110,19 +1066,24 @@ static meft_status route_impl(const meft_shape& s, const void* h, const void* Wg
     launch_gemm_nt(s, a, s.T, 1, "router_gemm", st);
   }
   const size_t stride = (size_t)s.T * s.n_blocks;
-#define PK(Z) MEFT_LAUNCH("route_pick", (route_pick_kernel<Z>), dim3((s.T + 3) / 4), dim3(256), 0, st, p, n_part, stride, bias, s.T, s.n_blocks, s.top_e, block_idx, block_score)
-  if (s.n_blocks <= 64) PK(1);
-  else if (s.n_blocks <= 128) PK(2);
-  else if (s.n_blocks <= 256) PK(4);
   // beyond 256 blocks the keys take sixteen registers per lane: better for several rounds on few tokens (route call, LDS
   // keys / registers, 1024 blocks and 2048 tokens: 39.9 / 28.7 us for 16 blocks, 23.4 / 22.2 for 4, 19.1 / 20.7 for 1),
   // worse once the tokens fill the chip (16384 tokens: 112 / 153, 55 / 104, 40 / 92)
-  else if (s.n_blocks <= 1024 && s.top_e >= 8 && s.T <= 2048) PK(16);
-  else
+  const bool many = s.n_blocks <= 1024 && s.top_e >= 8 && s.T <= 2048;
+#define PK(Z, KEEP) MEFT_LAUNCH("route_pick", (route_pick_kernel<Z, KEEP>), dim3((s.T + 3) / 4), dim3(256), 0, st, p, n_part, stride, bias, s.T, s.n_blocks, s.top_e, block_idx, block_score, scores)
+#define PICK(KEEP)                    \
+  if (s.n_blocks <= 64) PK(1, KEEP);  \
+  else if (s.n_blocks <= 128) PK(2, KEEP); \
+  else if (s.n_blocks <= 256) PK(4, KEEP); \
+  else if (many) PK(16, KEEP);        \
+  else MEFT_LAUNCH("route_topk", route_topk_kernel<KEEP>, dim3(s.T), dim3(64), (size_t)s.n_blocks * 4, st, p, n_part, stride, bias, s.n_blocks, s.top_e, block_idx, block_score, scores)
+  if (scores) {
+    PICK(true);
+  } else {
+    PICK(false);
+  }
+#undef PICK
 #undef PK
-  MEFT_LAUNCH("route_topk", route_topk_kernel, dim3(s.T), dim3(64), (size_t)s.n_blocks * 4, st, p, n_part,
-              (size_t)s.T * s.n_blocks, bias,
-              s.n_blocks, s.top_e, block_idx, block_score);
   return launch_status();
 }
 
@@ -1514,7 +1475,22 @@ meft_status meft_route(const meft_shape* shape, const void* h, const void* Wg, c
   hipStream_t st = static_cast<hipStream_t>(stream);
   MEFT_API_LOCK();
   clear_stale_error();
-  return route_impl(s, h, Wg, bias, block_idx, block_score, w.p, st);
+  return route_impl(s, h, Wg, bias, block_idx, block_score, nullptr, w.p, st);
+}
+
+meft_status meft_route_scores(const meft_shape* shape, const void* h, const void* Wg, const float* bias, int32_t* block_idx,
+                              float* block_score, float* scores, void* ws, size_t ws_bytes, void* stream) {
+  meft_status rc = check_shape(shape);
+  if (rc != MEFT_OK) return rc;
+  const meft_shape& s = *shape;
+  if (!h || !Wg || !block_idx || !scores || !aligned16(h) || !aligned16(Wg) || !aligned16(scores)) return MEFT_ERR_INVALID_ARG;
+  RouteWs w(s, ws);
+  if ((rc = check_ws(s, ws, ws_bytes)) != MEFT_OK) return rc;
+  if (s.T == 0) return MEFT_OK;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  MEFT_API_LOCK();
+  clear_stale_error();
+  return route_impl(s, h, Wg, bias, block_idx, block_score, scores, w.p, st);
 }
 
 // Address of `scratch` on the current device, looked up on the first call with that device current.
@@ -1546,7 +1522,7 @@ meft_status meft_route_static(const meft_shape* shape, const void* h, const void
   if (!p) { (void)launch_status(); return MEFT_ERR_DEVICE; }
   const bool timing = g_prof_on;   // per-kernel timing creates events: off inside this call
   g_prof_on = false;
-  rc = route_impl(s, h, Wg, bias, block_idx, block_score, p, st);
+  rc = route_impl(s, h, Wg, bias, block_idx, block_score, nullptr, p, st);
   g_prof_on = timing;
   return rc;
 }

@@ -79,10 +79,12 @@ __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
 // blocks l, l + 64, ... in registers; e rounds of a wave-wide maximum through DPP moves, its lowest block by ballots,
 // and the winner is retired by zeroing its key (a live key is never 0 for finite scores).  Output order: score
 // descending, block id ascending.  Against keys in LDS and 64-bit shuffles: 8.7 -> 5 us (8192 tokens, 64 blocks).
-template <int Z>
+// kKeep: the scores themselves are written too.
+template <int Z, bool kKeep>
 __global__ __launch_bounds__(256) void route_pick_kernel(const float* __restrict__ p, int n_part, size_t part_stride,
                                                          const float* __restrict__ bias, int n_tok, int B, int e,
-                                                         int32_t* __restrict__ block_idx, float* __restrict__ block_score) {
+                                                         int32_t* __restrict__ block_idx, float* __restrict__ block_score,
+                                                         float* __restrict__ scores) {
   const int lane = threadIdx.x & 63, t = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (t >= n_tok) return;
   const float* row = p + (size_t)t * B;
@@ -95,6 +97,7 @@ __global__ __launch_bounds__(256) void route_pick_kernel(const float* __restrict
       float v = row[b];
       for (int s = 1; s < n_part; ++s) v += row[s * part_stride + b];   // partial scores of a split contraction
       if (bias) v += bias[b];
+      if (kKeep) scores[(size_t)t * B + b] = v;
       key[z] = order_key(v);
     }
   }

@@ -11,11 +11,13 @@ namespace meft {
 // B scores sits in LDS as ordered keys; e rounds of a wave-wide arg-max, the winner is retired
 // by zeroing its key (a live key is never 0 for finite scores).  Output order: score descending,
 // block id ascending.  The scores may arrive as n_part partial sums, part_stride floats apart.
+// kKeep: the scores themselves are written too.
 // ---------------------------------------------------------------------------------------------
+template <bool kKeep>
 __global__ __launch_bounds__(64) void route_topk_kernel(const float* __restrict__ p, int n_part, size_t part_stride,
                                                         const float* __restrict__ bias, int B, int e,
                                                         int32_t* __restrict__ block_idx,
-                                                        float* __restrict__ block_score) {
+                                                        float* __restrict__ block_score, float* __restrict__ scores) {
   extern __shared__ uint32_t s_key[];
   const int t = blockIdx.x, lane = threadIdx.x;
   const float* row = p + (size_t)t * B;
@@ -23,6 +25,7 @@ __global__ __launch_bounds__(64) void route_topk_kernel(const float* __restrict_
     float v = row[b];
     for (int s = 1; s < n_part; ++s) v += row[s * part_stride + b];   // partial scores of a split contraction
     if (bias) v += bias[b];
+    if (kKeep) scores[(size_t)t * B + b] = v;
     s_key[b] = order_key(v);
   }
   __syncthreads();

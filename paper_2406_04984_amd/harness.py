@@ -1,4 +1,4 @@
-"""Device buffers of one layer and the three ABI calls on them.
+"""Device buffers of one layer and the three ABI calls on them; of one block of a network around it and its training step.
 
 Used by the benchmark and by the GPU tests.  PyTorch is here for device memory and the stream only;
 every step of the layer runs in libmeft through paper_2406_04984_amd.binding.  This module computes
@@ -143,3 +143,55 @@ class DeviceLayer:
                 r[name] = to_host(x.index_select(0, sel))
         r["grad_rows"] = None if rows is None else np.asarray(rows, np.int64)
         return r
+
+
+class DeviceBlock(DeviceLayer):
+    """A block of a network around the layer: h = norm(x), the sparse layer on h, y = x + dropout(out), and the router's balance
+    loss.  The inputs' h is taken as x, their dOut as the gradient of y."""
+
+    def __init__(self, t: synth.Tensors, norm="rms", eps=1e-5, p=0.1, seed=1, offset=0, balance=0.01, z=0.001, valid=None,
+                 binding=None):
+        torch = _torch()
+        super().__init__(t, binding)
+        B, c = self.B, self.cfg
+        self.hp_norm = B.MeftNorm({"layer": B.MEFT_NORM_LAYER, "rms": B.MEFT_NORM_RMS}[norm], eps)
+        self.hp_drop, self.hp_balance = B.MeftDrop(p, seed, offset), B.MeftBalance(balance, z)
+        f32, dev = torch.float32, "cuda"
+        self.step_count = torch.zeros((1,), dtype=torch.int64, device=dev)   # added to the dropout's offset
+        self.valid = None if valid is None else torch.as_tensor(np.asarray(valid, np.uint8)).cuda()
+        self.x, self.dy = self.h, self.dOut
+        self.h, self.dOut = torch.zeros_like(self.x), torch.zeros_like(self.dy)
+        self.gamma = torch.ones((c.d,), dtype=self.dt, device=dev)
+        self.beta = torch.zeros((c.d,), dtype=self.dt, device=dev) if norm == "layer" else None
+        self.mean, self.rstd = (torch.zeros((c.T,), dtype=f32, device=dev) for _ in range(2))
+        self.y, self.dx = torch.zeros_like(self.x), torch.zeros_like(self.x)
+        self.scores, self.dscores = (torch.zeros((c.T, c.n_blocks), dtype=f32, device=dev) for _ in range(2))
+        self.counts = torch.zeros((c.n_blocks,), dtype=torch.int32, device=dev)
+        self.n_valid = torch.zeros((1,), dtype=torch.int32, device=dev)
+        self.prob, self.loss = torch.zeros((c.n_blocks,), dtype=f32, device=dev), torch.zeros((3,), dtype=f32, device=dev)
+        self.dWg, self.dbias = torch.zeros_like(self.Wg), torch.zeros((c.n_blocks,), dtype=f32, device=dev)
+        self.dgamma = torch.zeros_like(self.gamma)
+        self.dbeta = None if self.beta is None else torch.zeros_like(self.beta)
+        self.block_ws = torch.empty((B.meft_block_workspace_bytes(self.shape),), dtype=torch.uint8, device=dev)
+
+    def forward(self):
+        B, s = self.B, self.shape
+        B.meft_norm_fwd(s, self.hp_norm, self.x, self.gamma, self.beta, self.h, self.mean, self.rstd)
+        B.meft_route_scores(s, self.h, self.Wg, self.bias, self.block_idx, self.block_score, self.scores, self.ws)
+        self.fwd()
+        B.meft_dropout_add(s, self.hp_drop, self.step_count, self.out, self.x, self.y)
+        B.meft_balance_fwd(s, self.hp_balance, self.scores, self.block_idx, self.valid, self.counts, self.n_valid, self.prob,
+                           self.loss, self.block_ws)
+
+    def backward(self):
+        B, s = self.B, self.shape
+        B.meft_dropout_add(s, self.hp_drop, self.step_count, self.dy, None, self.dOut)
+        self.bwd()
+        B.meft_balance_bwd(s, self.hp_balance, self.scores, self.counts, self.n_valid, self.valid, None, self.dscores)
+        B.meft_route_bwd(s, self.h, self.Wg, self.dscores, self.dh, self.dh, self.dWg, self.dbias, self.block_ws)
+        B.meft_norm_bwd(s, self.hp_norm, self.x, self.gamma, self.mean, self.rstd, self.dh, self.dy, self.dx, self.dgamma,
+                        self.dbeta, self.block_ws)
+
+    def step(self):
+        self.forward()
+        self.backward()

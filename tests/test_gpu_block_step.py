@@ -1,0 +1,131 @@
+"""A whole training step of a block around the layer, through the calls as a program makes them: each result against fp64 from
+the call's own inputs (their slacks are derived in the tests of the calls), captured and replayed, on other streams."""
+import numpy as np
+import pytest
+
+from oracle import block_ref as R
+from paper_2406_04984_amd import synth
+from tests.within import U, assert_within, host64
+
+pytestmark = pytest.mark.gpu
+
+CASES = [dict(T=150, d=72, n_blocks=6, block_size=40, top_e=2, top_k=12, dtype="f32", seed=1401),
+         dict(T=700, d=192, n_blocks=70, block_size=32, top_e=3, top_k=30, dtype="bf16", seed=1402),
+         dict(T=1, d=256, n_blocks=8, block_size=64, top_e=2, top_k=16, dtype="bf16", seed=1403)]
+IDS = ["f32", "bf16", "one_token"]
+OUTPUTS = ("h", "mean", "rstd", "block_idx", "scores", "out", "y", "counts", "n_valid", "prob", "loss", "dOut", "dscores", "dh", "dWg",
+           "dbias", "dx", "dgamma", "dbeta")
+
+
+def _block(kw, norm="layer", **more):
+    from paper_2406_04984_amd.harness import DeviceBlock
+    t = synth.make_inputs(synth.small_case(**kw))
+    T = kw["T"]
+    blk = DeviceBlock(t, norm=norm, seed=11, valid=None if T == 1 else np.arange(T) % 7 != 3, **more)
+    r = np.random.RandomState(5)
+    import torch
+    blk.gamma.copy_(torch.from_numpy(1 + 0.1 * r.standard_normal(kw["d"])))
+    if blk.beta is not None:
+        blk.beta.copy_(torch.from_numpy(0.1 * r.standard_normal(kw["d"])))
+    return blk
+
+
+def _outputs(blk):
+    return {n: getattr(blk, n).clone() for n in OUTPUTS if getattr(blk, n) is not None}
+
+
+@pytest.mark.parametrize("norm", ["layer", "rms"])
+@pytest.mark.parametrize("kw", CASES, ids=IDS)
+def test_step(kw, norm):
+    blk = _block(kw, norm, p=0.2, offset=3, balance=2.0, z=0.5)
+    blk.step_count.fill_(4)
+    blk.forward()
+    blk.backward()
+    T, d, e, layer = kw["T"], kw["d"], kw["top_e"], norm == "layer"
+    v = {n: host64(getattr(blk, n)) for n in OUTPUTS + ("x", "dy", "gamma", "Wg") if getattr(blk, n) is not None}
+    beta = None if blk.beta is None else host64(blk.beta)
+    gain = R.gain(T, d, 0.2, 11, 7)
+    assert_within("y", blk.y, v["x"] + gain * v["out"], 2 * U * (np.abs(v["x"]) + gain * np.abs(v["out"])))
+    assert_within("dOut", blk.dOut, gain * v["dy"], U * gain * np.abs(v["dy"]))
+    h, mean, rstd = R.norm_fwd(v["x"], v["gamma"], beta, layer, 1e-5)
+    A = 1 + np.abs(v["x"]).mean(1, keepdims=True) * rstd[:, None]
+    xh = (v["x"] - mean[:, None]) * rstd[:, None]
+    assert_within("h", blk.h, h, 64 * U * ((np.abs(xh) + 1) * np.abs(v["gamma"]) * A + (0 if beta is None else np.abs(beta))))
+    valid = None if blk.valid is None else blk.valid.cpu().numpy()
+    idx = blk.block_idx.cpu().numpy()
+    counts, n, prob, loss = R.balance_fwd(v["scores"], idx, valid, 2.0, 0.5)
+    assert np.array_equal(counts, v["counts"]) and n == int(v["n_valid"][0])
+    assert_within("loss", blk.loss, loss, (T + 200) * U * np.abs(loss))
+    ds = R.balance_bwd(v["scores"], counts, n, e, valid, 2.0, 0.5, 1.0)
+    assert_within("dscores", blk.dscores, ds, 200 * U * np.abs(ds).max())
+    # what meft_sparse_bwd gave before the router's part was added
+    extra = v["dscores"] @ v["Wg"]
+    dh_sparse = blk.dh.clone()
+    blk.bwd()
+    sparse = host64(blk.dh)
+    assert np.abs(extra).max() > 0 or T == 1
+    half = 2.0 ** -16 if kw["dtype"] == "bf16" else 0
+    assert_within("dh", dh_sparse, sparse + extra, (half + 2 * U * (kw["n_blocks"] + 32)) * (np.abs(v["dscores"]) @ np.abs(v["Wg"])) +
+                  2 * U * np.abs(sparse))
+    dWg, dbias = R.route_bwd(v["h"], v["Wg"], v["dscores"], None)[1:]
+    assert_within("dWg", blk.dWg, dWg, (half + 2 * U * (T + 32)) * (np.abs(v["dscores"]).T @ np.abs(v["h"])))
+    assert_within("dbias", blk.dbias, dbias, (T + 32) * U * np.abs(v["dscores"]).sum(0))
+    m, r = v["mean"], v["rstd"]
+    dx, dgamma, dbeta = R.norm_bwd(v["x"], v["gamma"], m, r, v["dh"], v["dy"], layer)
+    xh, g = (v["x"] - m[:, None]) * r[:, None], v["dh"] * v["gamma"]
+    assert_within("dx", blk.dx, dx, 64 * U * (r[:, None] * (np.abs(g) + np.abs(g).mean(1, keepdims=True) + np.abs(xh) *
+                                              np.abs(g * xh).mean(1, keepdims=True)) + np.abs(v["dy"])))
+    assert_within("dgamma", blk.dgamma, dgamma, (T + 32) * U * np.abs(v["dh"] * xh).sum(0))
+    if layer:
+        assert_within("dbeta", blk.dbeta, dbeta, (T + 32) * U * np.abs(v["dh"]).sum(0))
+
+
+@pytest.mark.parametrize("kw", CASES, ids=IDS)
+def test_replays_of_a_captured_step(kw):
+    """Every replay gives what the eager step gives with the same counter, with eager work of the program in between."""
+    import torch
+    blk = _block(kw)
+    want = []
+    for count in (0, 1, 2):
+        blk.step_count.fill_(count)
+        blk.step()
+        torch.cuda.synchronize()
+        want.append(_outputs(blk))
+    if kw["T"] > 1:
+        assert not torch.equal(want[0]["y"], want[1]["y"])      # another mask each step
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        blk.step()
+    for rep, count in enumerate((1, 0, 2, 1)):
+        for n in OUTPUTS:
+            if getattr(blk, n) is not None:
+                getattr(blk, n).fill_(3)
+        blk.ws.fill_(0xFF if rep % 2 else 0x00)
+        blk.block_ws.fill_(0x00 if rep % 2 else 0xFF)
+        blk.step_count.fill_(count)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        got = _outputs(blk)
+        assert all(torch.equal(got[n], want[count][n]) for n in got), (rep, [n for n in got if not torch.equal(got[n], want[count][n])])
+
+
+def test_two_streams_at_once():
+    """Two blocks on two streams, their calls interleaved: nothing that they share stands between them."""
+    import torch
+    a, b = _block(CASES[1]), _block(CASES[0])
+    want = []
+    for blk in (a, b):
+        blk.step()
+        torch.cuda.synchronize()
+        want.append(_outputs(blk))
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):
+        for part in ("forward", "backward"):
+            for blk, st in ((a, s1), (b, s2)):
+                with torch.cuda.stream(st):
+                    getattr(blk, part)()
+    torch.cuda.synchronize()
+    for blk, w in zip((a, b), want):
+        got = _outputs(blk)
+        assert all(torch.equal(got[n], w[n]) for n in got)
