@@ -195,17 +195,17 @@ bool balance_ok(const meft_balance* b) { return b && std::isfinite(b->balance) &
 
 // ---- router gradient ------------------------------------------------------------------------
 struct RouteGradPlan {
-  int slices, m, m_waves, groups, splits, per_split;
+  int slices, m_shift, groups, splits, per_split;
 };
 RouteGradPlan route_grad_plan(const meft_shape& s) {
   RouteGradPlan p{};
   p.slices = (s.d + kRgCols - 1) / kRgCols;
-  p.m = s.n_blocks <= 32 ? 1 : 2;
-  const int tiles = (s.n_blocks + 32 * p.m - 1) / (32 * p.m);
-  p.m_waves = tiles >= 3 ? 4 : tiles;
-  p.groups = (tiles + p.m_waves - 1) / p.m_waves;
-  // as many splits of the tokens as give every compute unit a workgroup, each at least four steps of 16 tokens per wave
-  const int64_t least = 16 * (4 / p.m_waves) * 4, want = (kCus + p.slices * p.groups - 1) / (p.slices * p.groups);
+  const int tiles = (s.n_blocks + 31) / 32;
+  while ((1 << p.m_shift) < tiles && (1 << p.m_shift) < kRgWaves) ++p.m_shift;
+  const int m_waves = 1 << p.m_shift;
+  p.groups = (tiles + m_waves - 1) / m_waves;
+  // as many splits of the tokens as give every compute unit a workgroup, each at least 16 tokens per wave
+  const int64_t least = 16 * (kRgWaves / m_waves), want = (kCus + p.slices * p.groups - 1) / (p.slices * p.groups);
   const int64_t can = (s.T + least - 1) / least;
   int64_t splits = want < can ? want : can;
   if (splits < 1) splits = 1;
@@ -234,16 +234,21 @@ meft_status route_bwd(const meft_shape& s, const void* h, const void* Wg, const 
   const RouteGradPlan p = route_grad_plan(s);
   const RouteGradWs w(s, ws);
   const RouteGradArgs<T> a{static_cast<const T*>(h), static_cast<const T*>(Wg), static_cast<const T*>(add), ds, static_cast<T*>(dh),
-                           static_cast<T*>(dWg), dbias, w.part, w.part_bias, s.T, s.d, s.n_blocks, p.slices, p.m_waves, p.splits,
+                           static_cast<T*>(dWg), dbias, w.part, w.part_bias, s.T, s.d, s.n_blocks, p.slices, p.m_shift, p.splits,
                            p.per_split};
   if (dh && s.T > 0) {
-    const int64_t tiles = ((int64_t)s.T + 4 * kRgTok - 1) / (4 * kRgTok);
-    MEFT_LAUNCH("route_dh", route_dh_kernel<T>, dim3((unsigned)(tiles * p.slices)), dim3(256), 0, st, a);
+    static std::once_flag configured;   // up to kDhLds of the router
+    std::call_once(configured, [] {
+      (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&route_dh_kernel<T>), hipFuncAttributeMaxDynamicSharedMemorySize, kDhLds);
+    });
+    const int step = dh_step_bytes<T>(), all = (s.n_blocks + 15) / 16 * step, lds = all < kDhLds ? all : kDhLds;
+    const int64_t rounds = ((int64_t)s.T + 32 * kDhWaves - 1) / (32 * kDhWaves), most = (2 * kCus + p.slices - 1) / p.slices;
+    const dim3 grid((unsigned)(rounds < most ? rounds : most), p.slices);
+    MEFT_LAUNCH("route_dh", route_dh_kernel<T>, grid, dim3(64 * kDhWaves), lds, st, a);
   }
   if (dWg || dbias) {
-    const dim3 grid(dWg ? p.slices : 1, p.groups, p.splits);
-    if (p.m == 1) MEFT_LAUNCH("route_dw", (route_dw_kernel<T, 1>), grid, dim3(256), 0, st, a);
-    else MEFT_LAUNCH("route_dw", (route_dw_kernel<T, 2>), grid, dim3(256), 0, st, a);
+    const dim3 grid(p.splits, dWg ? p.slices : 1, p.groups);
+    MEFT_LAUNCH("route_dw", route_dw_kernel<T>, grid, dim3(64 * kRgWaves), 0, st, a);
     if (p.splits > 1) {
       const int64_t quads = dWg ? (int64_t)s.n_blocks * s.d / 4 : 0;
       MEFT_LAUNCH("route_dw_join", route_dw_join_kernel<T>, dim3((unsigned)((quads + 255) / 256 + 1)), dim3(256), 0, st, a);

@@ -15,16 +15,21 @@
 
 namespace meft {
 
-typedef u32x2 u32x2_8 __attribute__((aligned(8)));
-
 // eight rows of four columns, and the operands that they give
 template <typename T>
 struct Rows8;
 
 template <>
 struct Rows8<bf16_t> {
-  u32x2 w[8];
-  __device__ __forceinline__ void load(int u, const bf16_t* p) { w[u] = *reinterpret_cast<const u32x2*>(p); }
+  typedef u32x2 Quad;
+  Quad w[8];
+  static __device__ __forceinline__ Quad load(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+    return __builtin_bit_cast(Quad, __builtin_amdgcn_raw_buffer_load_b64(r, (int)at, 0, 0));
+  }
+  static __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t r, uint32_t at, const float (&v)[4]) {
+    const Quad q = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    __builtin_amdgcn_raw_buffer_store_b64(q, r, (int)at, 0, 2);
+  }
   // the eight rows of column j
   __device__ __forceinline__ bf16x8 operand(int j) const {
     u32x4 r;
@@ -33,22 +38,41 @@ struct Rows8<bf16_t> {
       r[i] = __builtin_amdgcn_perm(w[2 * i + 1][j / 2], w[2 * i][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
     return __builtin_bit_cast(bf16x8, r);
   }
+  static __device__ __forceinline__ void widen(Quad q, float (&v)[4]) {
+    v[0] = __uint_as_float(q.x << 16); v[1] = __uint_as_float(q.x & 0xFFFF0000u);
+    v[2] = __uint_as_float(q.y << 16); v[3] = __uint_as_float(q.y & 0xFFFF0000u);
+  }
 };
 
 template <>
 struct Rows8<float> {
-  f32x4 w[8];
-  __device__ __forceinline__ void load(int u, const float* p) { w[u] = *reinterpret_cast<const f32x4*>(p); }
+  typedef f32x4 Quad;
+  Quad w[8];
+  static __device__ __forceinline__ Quad load(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+    return __builtin_bit_cast(Quad, __builtin_amdgcn_raw_buffer_load_b128(r, (int)at, 0, 0));
+  }
+  static __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t r, uint32_t at, const float (&v)[4]) {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]}), r, (int)at, 0, 0);
+  }
+  static __device__ __forceinline__ void widen(Quad q, float (&v)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = q[j];
+  }
 };
 
-// acc[j] += a (8 values of a row of the left operand per lane) * rows, for the four columns j
-__device__ __forceinline__ void mma_rows8(const float (&a)[8], const Rows8<bf16_t>& rows, f32x16 (&acc)[4]) {
-  u32x4 hi, lo;
+// the two bf16 parts of eight values
+__device__ __forceinline__ void split(const float (&a)[8], u32x4& hi, u32x4& lo) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     hi[i] = pack_bf16x2(a[2 * i], a[2 * i + 1]);
     lo[i] = pack_bf16x2(a[2 * i] - __uint_as_float(hi[i] << 16), a[2 * i + 1] - __uint_as_float(hi[i] & 0xFFFF0000u));
   }
+}
+
+// acc[j] += a (8 values of a row of the left operand per lane) * rows, for the four columns j
+__device__ __forceinline__ void mma_rows8(const float (&a)[8], const Rows8<bf16_t>& rows, f32x16 (&acc)[4]) {
+  u32x4 hi, lo;
+  split(a, hi, lo);
   const bf16x8 h8 = __builtin_bit_cast(bf16x8, hi), l8 = __builtin_bit_cast(bf16x8, lo);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -68,7 +92,6 @@ __device__ __forceinline__ void mma_rows8(const float (&a)[8], const Rows8<float
 __device__ __forceinline__ int tile_row(int r, int lane) { return 8 * (r / 4) + 4 * (lane / 32) + r % 4; }
 
 constexpr int kRgCols = 128;    // columns of a wave's tile
-constexpr int kRgTok = 64;      // dh: tokens of a wave's tile
 
 template <typename T>
 struct RouteGradArgs {
@@ -78,7 +101,7 @@ struct RouteGradArgs {
   float *dbias, *part, *part_bias;   // part: [split][B][d], where there is more than one split
   int n_tok, d, B;
   int slices;                        // ceil(d / kRgCols)
-  int m_waves, splits, per_split;    // dWg: waves along the blocks, splits of the tokens, tokens of a split (a multiple of 16)
+  int m_shift, splits, per_split;    // dWg: 2^m_shift waves along the blocks, splits of the tokens, tokens of a split (a multiple of 16)
 };
 
 template <typename T>
@@ -86,183 +109,261 @@ __device__ __forceinline__ void store4(T* p, const float (&v)[4]) {
   if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
   else *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
 }
+// `rows` rows of `row_bytes` bytes from `base` on, which is the same in all lanes: what lies behind reads as 0 and is not
+// written.  The rows of a tile, so far below 4 GB.
 template <typename T>
-__device__ __forceinline__ void load4(const T* p, float (&v)[4]) {
-  if constexpr (sizeof(T) == 2) {
-    const u32x2 w = *reinterpret_cast<const u32x2*>(p);
-    v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xFFFF0000u);
-    v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xFFFF0000u);
-  } else {
-    const f32x4 w = *reinterpret_cast<const f32x4*>(p);
-    v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
-  }
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const T* base, int rows, uint32_t row_bytes) {
+  // the compiler does not always see that they are, and would then loop over the lanes
+  const uint64_t p = reinterpret_cast<uint64_t>(base);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)p), hi = __builtin_amdgcn_readfirstlane((uint32_t)(p >> 32));
+  const int bytes = __builtin_amdgcn_readfirstlane((int)(max(rows, 0) * row_bytes));
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((uint64_t)hi << 32 | lo), 0, bytes, 0x00020000);
 }
+constexpr uint32_t kNoColumn = 0xF0000000u;   // an offset behind the rows of any tile, also with a row's offset added
 
-// dh.  A wave: 64 tokens x 128 columns; the four waves of a workgroup take consecutive tokens of the same columns, whose
-// router rows they then find in the vector cache.  Grid: slices * ceil(T / 256), the slices fastest.
+// A step of 16 blocks of the router in LDS, as the matrix instructions want it: kUnits words of 16 bytes per lane.
 template <typename T>
-__global__ __launch_bounds__(256) void route_dh_kernel(RouteGradArgs<T> a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
-  const int tile = blockIdx.x / a.slices, slice = blockIdx.x - tile * a.slices;
-  const int64_t t0 = (int64_t)tile * 4 * kRgTok + wave * kRgTok;
-  if (t0 >= a.n_tok) return;
-  const int c = slice * kRgCols + 4 * (lane & 31), cc = min(c, a.d - 4);
-  const float* ds[2];
+struct StepWords;
+template <>
+struct StepWords<bf16_t> {
+  static constexpr int kUnits = 4;   // one per column j: its eight rows
+  static __device__ __forceinline__ void put(u32x4* lds, const Rows8<bf16_t>& w, int lane) {
 #pragma unroll
-  for (int m = 0; m < 2; ++m) ds[m] = a.ds + (size_t)min(t0 + m * 32 + (lane & 31), (int64_t)a.n_tok - 1) * a.B;
-  f32x16 acc[2][4];
+    for (int j = 0; j < 4; ++j) lds[j * 64 + lane] = __builtin_bit_cast(u32x4, w.operand(j));
+  }
+  static __device__ __forceinline__ void mma(const float (&x)[8], const u32x4* lds, int lane, f32x16 (&acc)[4]) {
+    u32x4 hi, lo;
+    split(x, hi, lo);
 #pragma unroll
-  for (int m = 0; m < 2; ++m)
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[m][j][r] = 0.f;
-  int b0 = 0;
-  for (; b0 + 16 <= a.B; b0 += 16) {
-    const int b = b0 + 8 * half;
-    Rows8<T> rows;
-#pragma unroll
-    for (int u = 0; u < 8; ++u) rows.load(u, a.Wg + (size_t)(b + u) * a.d + cc);
-#pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      float x[8];
-      *reinterpret_cast<u32x4*>(x) = *reinterpret_cast<const u32x4_dw*>(ds[m] + b);
-      *reinterpret_cast<u32x4*>(x + 4) = *reinterpret_cast<const u32x4_dw*>(ds[m] + b + 4);
-      mma_rows8(x, rows, acc[m]);
+    for (int j = 0; j < 4; ++j) {
+      const bf16x8 b = __builtin_bit_cast(bf16x8, lds[j * 64 + lane]);
+      acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, hi), b, acc[j], 0, 0, 0);
+      acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, lo), b, acc[j], 0, 0, 0);
     }
   }
-  if (b0 < a.B) {
-    const int b = b0 + 8 * half;
-    Rows8<T> rows;
+};
+template <>
+struct StepWords<float> {
+  static constexpr int kUnits = 8;   // one per row u: its four columns
+  static __device__ __forceinline__ void put(u32x4* lds, const Rows8<float>& w, int lane) {
 #pragma unroll
-    for (int u = 0; u < 8; ++u) rows.load(u, a.Wg + (size_t)min(b + u, a.B - 1) * a.d + cc);
-#pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      float x[8];
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const float v = ds[m][min(b + u, a.B - 1)];
-        x[u] = b + u < a.B ? v : 0.f;
-      }
-      mma_rows8(x, rows, acc[m]);
-    }
+    for (int u = 0; u < 8; ++u) lds[u * 64 + lane] = __builtin_bit_cast(u32x4, w.w[u]);
   }
-  if (c >= a.d) return;
-#pragma unroll
-  for (int m = 0; m < 2; ++m)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int64_t t = t0 + m * 32 + tile_row(r, lane);
-      if (t >= a.n_tok) continue;
-      float v[4] = {acc[m][0][r], acc[m][1][r], acc[m][2][r], acc[m][3][r]};
-      if (a.add) {
-        float x[4];
-        load4(a.add + (size_t)t * a.d + c, x);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] += x[j];
-      }
-      store4(a.dh + (size_t)t * a.d + c, v);
-    }
-}
-
-// dWg and dbias.  A wave: 32 M blocks x 128 columns over a share of the tokens, 16 at a time; a_waves waves lie along the
-// blocks, the others share out the tokens and are added through LDS.  Grid: (slices, ceil(B / (32 M m_waves)), splits).
-template <typename T, int M>
-__global__ __launch_bounds__(256) void route_dw_kernel(RouteGradArgs<T> a) {
-  __shared__ float s_acc[2][M * 64][64];
-  __shared__ float s_bias[4][M][32];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
-  const int m_waves = a.m_waves, k_waves = 4 / m_waves, mw = wave % m_waves, kw = wave / m_waves;
-  const int b0 = ((int)blockIdx.y * m_waves + mw) * 32 * M;
-  const int c = blockIdx.x * kRgCols + 4 * (lane & 31), cc = min(c, a.d - 4);
-  const int64_t begin = (int64_t)blockIdx.z * a.per_split, end = min(begin + a.per_split, (int64_t)a.n_tok);
-  int bb[M];
-#pragma unroll
-  for (int m = 0; m < M; ++m) bb[m] = min(b0 + 32 * m + (lane & 31), a.B - 1);
-  f32x16 acc[M][4];
-  float bias[M];
-#pragma unroll
-  for (int m = 0; m < M; ++m) {
-    bias[m] = 0.f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[m][j][r] = 0.f;
-  }
-  for (int64_t t0 = begin + 16 * kw; t0 < end; t0 += 16 * k_waves) {
-    const int64_t t = t0 + 8 * half;
-    Rows8<T> rows;
-    float x[M][8];
-    const bool whole = t0 + 16 <= end;
+  static __device__ __forceinline__ void mma(const float (&x)[8], const u32x4* lds, int lane, f32x16 (&acc)[4]) {
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      const int64_t tt = whole ? t + u : min(t + u, end - 1);
-      rows.load(u, a.h + (size_t)tt * a.d + cc);
+      const f32x4 b = __builtin_bit_cast(f32x4, lds[u * 64 + lane]);
 #pragma unroll
-      for (int m = 0; m < M; ++m) x[m][u] = a.ds[(size_t)tt * a.B + bb[m]];
+      for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[u], b[j], acc[j], 0, 0, 0);
     }
-    if (!whole) {
+  }
+};
+
+constexpr int kDhWaves = 4;
+constexpr int kDhLds = 128 << 10;   // most of LDS that a workgroup's part of the router takes
+template <typename T>
+constexpr int dh_step_bytes() { return StepWords<T>::kUnits * 64 * 16; }
+
+// dh.  A workgroup holds the router's rows of 128 columns in LDS, as operands, and walks tiles of 32 tokens per wave.  What is
+// added to a tile and its ds are asked for while the tile before is computed.  More blocks than kDhLds holds are staged piece
+// by piece for every tile.  Grid: (workgroups along the tokens, slices): the slices of the same tokens share an XCD's L2, as far as
+// the workgroups along the tokens are a multiple of 8.
+template <typename T>
+__global__ __launch_bounds__(64 * kDhWaves, 2) void route_dh_kernel(RouteGradArgs<T> a) {
+  typedef Rows8<T> Rows;
+  typedef StepWords<T> Words;
+  extern __shared__ u32x4 s_w[];
+  constexpr int kMaxSteps = kDhLds / dh_step_bytes<T>();
+  const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = blockIdx.y * kRgCols + 4 * col;
+  const uint32_t row_bytes = a.d * (uint32_t)sizeof(T), c_bytes = (uint32_t)min(c, a.d - 4) * (uint32_t)sizeof(T);
+  const int steps = (a.B + 15) / 16;
+  const uint32_t o = 4 * half * row_bytes + (c < a.d ? c_bytes : kNoColumn);
+  const uint32_t ds_off = (uint32_t)col * a.B * 4u + 32u * half;
+
+  auto stage = [&](int first, int n) {   // steps first .. first + n - 1 of the router
+    for (int s = wave; s < n; s += kDhWaves) {
+      const int b0 = (first + s) * 16;
+      const __amdgpu_buffer_rsrc_t wg = rows_at(a.Wg + (size_t)b0 * a.d, min(a.B - b0, 16), row_bytes);
+      Rows w;
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
-#pragma unroll
-        for (int m = 0; m < M; ++m) x[m][u] = t + u < end ? x[m][u] : 0.f;
+      for (int u = 0; u < 8; ++u) w.w[u] = Rows::load(wg, 8 * half * row_bytes + c_bytes + u * row_bytes);
+      Words::put(s_w + s * Words::kUnits * 64, w, lane);
     }
+  };
+  // eight values of ds of this lane's token; blocks and tokens that are not there are 0
+  auto load_ds = [&](__amdgpu_buffer_rsrc_t ds, int s, u32x4(&x)[2]) {
+    const int b = 16 * s + 8 * half;
+    if ((a.B & 3) == 0) {
 #pragma unroll
-    for (int m = 0; m < M; ++m) {
-      mma_rows8(x[m], rows, acc[m]);
-      if (blockIdx.x == 0) bias[m] += ((x[m][0] + x[m][1]) + (x[m][2] + x[m][3])) + ((x[m][4] + x[m][5]) + (x[m][6] + x[m][7]));
+      for (int i = 0; i < 2; ++i)
+        x[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ds, (int)(b + 4 * i < a.B ? ds_off + 64 * s + 16 * i : kNoColumn), 0, 0));
+    } else {   // a word of four might run over the row's end
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u / 4][u % 4] = __builtin_amdgcn_raw_buffer_load_b32(ds, (int)(b + u < a.B ? ds_off + 64 * s + 4 * u : kNoColumn), 0, 0);
+    }
+  };
+  const int64_t tile0 = (int64_t)blockIdx.x * kDhWaves + wave, n_tiles = ((int64_t)a.n_tok + 31) / 32;
+  const int stride = gridDim.x * kDhWaves;
+  auto tile_rows = [&](int64_t tile) { return (int)max((int64_t)0, min((int64_t)32, a.n_tok - tile * 32)); };
+  auto ds_of = [&](int64_t tile) { return rows_at(a.ds + (size_t)tile * 32 * a.B, tile_rows(tile), a.B * 4u); };
+
+  typename Rows::Quad y[16];   // 0 where nothing is added
+  auto load_add = [&](int64_t tile) {
+    const __amdgpu_buffer_rsrc_t add = rows_at(a.add + (a.add ? (size_t)tile * 32 * a.d : 0), a.add ? tile_rows(tile) : 0, row_bytes);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) y[r] = Rows::load(add, o + (uint32_t)tile_row(r, 0) * row_bytes);
+  };
+  constexpr int kAhead = 4;   // steps of ds in registers or on their way
+  u32x4 x[kAhead][2];
+  const int pieces = (steps + kMaxSteps - 1) / kMaxSteps;
+  if (pieces == 1) stage(0, steps);
+  {
+    const __amdgpu_buffer_rsrc_t ds = ds_of(tile0);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) load_ds(ds, i, x[i]);
+  }
+  load_add(tile0);
+  if (pieces == 1) __syncthreads();
+  // every wave of the workgroup makes as many rounds as the first: there may be barriers in them
+  for (int64_t tile = tile0; tile - wave < n_tiles; tile += stride) {
+    const __amdgpu_buffer_rsrc_t ds = ds_of(tile), ds_next = ds_of(tile + stride);
+    f32x16 acc[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[j][r] = 0.f;
+    for (int p = 0; p < pieces; ++p) {
+      const int first = p * kMaxSteps, n = min(steps - first, kMaxSteps);
+      if (pieces > 1) {
+        __syncthreads();
+        stage(first, n);
+        __syncthreads();
+      }
+      for (int s0 = 0; s0 < n; s0 += kAhead) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          float f[8];
+#pragma unroll
+          for (int z = 0; z < 8; ++z) f[z] = __uint_as_float(x[i][z / 4][z % 4]);
+          // the next use of this place: later in the row, or the beginning of the next tile's
+          const int next = first + s0 + i + kAhead;
+          const bool same = first + s0 + kAhead < steps;
+          load_ds(same ? ds : ds_next, same ? next : i, x[i]);
+          if (i == 0 || s0 + i < n) Words::mma(f, s_w + (s0 + i) * Words::kUnits * 64, lane, acc);
+        }
+      }
+    }
+    const __amdgpu_buffer_rsrc_t to = rows_at(a.dh + (size_t)tile * 32 * a.d, tile_rows(tile), row_bytes);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      float v[4];
+      Rows::widen(y[r], v);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] += acc[j][r];
+      Rows::store(to, o + (uint32_t)tile_row(r, 0) * row_bytes, v);
+    }
+    load_add(tile + stride);
+  }
+}
+
+constexpr int kRgWaves = 8;
+
+// dWg and dbias.  A wave: 32 blocks x 128 columns over a share of the tokens, 16 at a time, the next step's operands on their
+// way; m_waves waves lie along the blocks, the others share out the tokens and are added through LDS.
+// Grid: (splits, slices, ceil(B / (32 m_waves))), so that the slices of the same tokens share an XCD's L2 (see route_dh_kernel).
+template <typename T>
+__global__ __launch_bounds__(64 * kRgWaves) void route_dw_kernel(RouteGradArgs<T> a) {
+  typedef Rows8<T> Rows;
+  __shared__ float s_acc[kRgWaves / 2][64][64];
+  __shared__ float s_bias[kRgWaves][32];
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int m_waves = 1 << a.m_shift, k_waves = kRgWaves >> a.m_shift, mw = wave & (m_waves - 1), kw = wave >> a.m_shift;
+  const int b0 = ((int)blockIdx.z * m_waves + mw) * 32;
+  const int c = blockIdx.y * kRgCols + 4 * (lane & 31);
+  const int64_t begin = (int64_t)blockIdx.x * a.per_split;
+  const int len = (int)min((int64_t)a.per_split, a.n_tok - begin);   // tokens of this split
+  const uint32_t row_bytes = a.d * (uint32_t)sizeof(T), ds_bytes = a.B * 4u;
+  const uint32_t h_off = 8 * half * row_bytes + (uint32_t)min(c, a.d - 4) * (uint32_t)sizeof(T);
+  const uint32_t ds_off = 8 * half * ds_bytes + (uint32_t)min(b0 + (lane & 31), a.B - 1) * 4u;
+  f32x16 acc[4];
+  float bias = 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[j][r] = 0.f;
+  constexpr int kAhead = 2;   // steps whose operands are in registers or on their way
+  Rows rows[kAhead];
+  float x[kAhead][8];
+  const int stride = 16 * k_waves;
+  auto load = [&](int t0, Rows& w, float(&v)[8]) {   // tokens that are not there are 0
+    const int left = min(len - t0, 16);
+    const __amdgpu_buffer_rsrc_t h = rows_at(a.h + (size_t)(begin + t0) * a.d, left, row_bytes);
+    const __amdgpu_buffer_rsrc_t ds = rows_at(a.ds + (size_t)(begin + t0) * a.B, left, ds_bytes);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      w.w[u] = Rows::load(h, h_off + u * row_bytes);
+      v[u] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(ds, (int)(ds_off + u * ds_bytes), 0, 0));
+    }
+  };
+  auto step = [&](const Rows& w, const float(&v)[8]) {
+    mma_rows8(v, w, acc);
+    bias += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead - 1; ++i) load(16 * kw + i * stride, rows[i], x[i]);
+  for (int t0 = 16 * kw; t0 < len; t0 += kAhead * stride) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      load(t0 + (i + kAhead - 1) * stride, rows[(i + kAhead - 1) % kAhead], x[(i + kAhead - 1) % kAhead]);
+      if (i == 0 || t0 + i * stride < len) step(rows[i], x[i]);
     }
   }
   // the waves that shared out the tokens, in pairs
   for (int n = k_waves / 2; n > 0; n /= 2) {
     __syncthreads();
-    float(*s)[64] = s_acc[(kw % n) * m_waves + mw];
+    float(*s)[64] = s_acc[(kw & (n - 1)) * m_waves + mw];
     if (kw >= n && kw < 2 * n) {
 #pragma unroll
-      for (int m = 0; m < M; ++m)
+      for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[(m * 4 + j) * 16 + r][lane] = acc[m][j][r];
+        for (int r = 0; r < 16; ++r) s[j * 16 + r][lane] = acc[j][r];
     }
     __syncthreads();
     if (kw < n) {
 #pragma unroll
-      for (int m = 0; m < M; ++m)
+      for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[m][j][r] += s[(m * 4 + j) * 16 + r][lane];
+        for (int r = 0; r < 16; ++r) acc[j][r] += s[j * 16 + r][lane];
     }
   }
-  if (blockIdx.x == 0) {
-#pragma unroll
-    for (int m = 0; m < M; ++m) {
-      const float v = bias[m] + __shfl_xor(bias[m], 32, kWave);
-      if (half == 0) s_bias[wave][m][lane] = v;
-    }
+  if (blockIdx.y == 0) {
+    bias += __shfl_xor(bias, 32, kWave);
+    if (half == 0) s_bias[wave][lane] = bias;
     __syncthreads();
     if (kw == 0 && half == 0 && a.dbias) {
-#pragma unroll
-      for (int m = 0; m < M; ++m) {
-        const int b = b0 + 32 * m + lane;
-        float v = 0.f;
-        for (int k = 0; k < k_waves; ++k) v += s_bias[k * m_waves + mw][m][lane];
-        if (b < a.B) (a.splits > 1 ? a.part_bias + (size_t)blockIdx.z * a.B : a.dbias)[b] = v;
-      }
+      float v = 0.f;
+      for (int k = 0; k < k_waves; ++k) v += s_bias[k * m_waves + mw][lane];
+      if (b0 + lane < a.B) (a.splits > 1 ? a.part_bias + (size_t)blockIdx.x * a.B : a.dbias)[b0 + lane] = v;
     }
   }
-  if (kw != 0 || c >= a.d || !a.dWg) return;
+  if (kw != 0 || !a.dWg) return;
+  const int left = min(a.B - b0, 32);
+  if (a.splits > 1) {
+    const __amdgpu_buffer_rsrc_t to = rows_at(a.part + ((size_t)blockIdx.x * a.B + b0) * a.d, left, a.d * 4u);
+    const uint32_t o = 4 * half * a.d * 4u + (c < a.d ? c * 4u : kNoColumn);
 #pragma unroll
-  for (int m = 0; m < M; ++m)
+    for (int r = 0; r < 16; ++r)
+      Rows8<float>::store(to, o + (uint32_t)tile_row(r, 0) * a.d * 4u, {acc[0][r], acc[1][r], acc[2][r], acc[3][r]});
+  } else {
+    const __amdgpu_buffer_rsrc_t to = rows_at(a.dWg + (size_t)b0 * a.d, left, row_bytes);
+    const uint32_t o = 4 * half * row_bytes + (c < a.d ? c * (uint32_t)sizeof(T) : kNoColumn);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int b = b0 + 32 * m + tile_row(r, lane);
-      if (b >= a.B) continue;
-      const float v[4] = {acc[m][0][r], acc[m][1][r], acc[m][2][r], acc[m][3][r]};
-      if (a.splits > 1) store4(a.part + ((size_t)blockIdx.z * a.B + b) * a.d + c, v);
-      else store4(a.dWg + (size_t)b * a.d + c, v);
-    }
+    for (int r = 0; r < 16; ++r)
+      Rows::store(to, o + (uint32_t)tile_row(r, 0) * row_bytes, {acc[0][r], acc[1][r], acc[2][r], acc[3][r]});
+  }
 }
 
 // the splits of dWg and dbias added up, in order; one workgroup more than dWg's quadruples need writes dbias
@@ -278,8 +379,7 @@ __global__ __launch_bounds__(256) void route_dw_join_kernel(RouteGradArgs<T> a) 
   if (i >= n || !a.dWg) return;
   float v[4] = {0.f, 0.f, 0.f, 0.f};
   for (int s = 0; s < a.splits; ++s) {
-    float x[4];
-    load4(a.part + (size_t)s * n + i, x);
+    const f32x4 x = *reinterpret_cast<const f32x4*>(a.part + (size_t)s * n + i);
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] += x[j];
   }
