@@ -194,18 +194,20 @@ void launch_balance_part(const meft_shape& s, const float* scores, const int32_t
 bool balance_ok(const meft_balance* b) { return b && std::isfinite(b->balance) && std::isfinite(b->z); }
 
 // ---- router gradient ------------------------------------------------------------------------
+constexpr int kDwWgs = kCus;   // workgroups of dWg to aim at
 struct RouteGradPlan {
-  int slices, m_shift, groups, splits, per_split;
+  int slices, m, m_shift, groups, splits, per_split;
 };
 RouteGradPlan route_grad_plan(const meft_shape& s) {
   RouteGradPlan p{};
   p.slices = (s.d + kRgCols - 1) / kRgCols;
-  const int tiles = (s.n_blocks + 31) / 32;
+  p.m = s.n_blocks <= 32 ? 1 : 2;
+  const int tiles = (s.n_blocks + 32 * p.m - 1) / (32 * p.m);
   while ((1 << p.m_shift) < tiles && (1 << p.m_shift) < kRgWaves) ++p.m_shift;
   const int m_waves = 1 << p.m_shift;
   p.groups = (tiles + m_waves - 1) / m_waves;
   // as many splits of the tokens as give every compute unit a workgroup, each at least 16 tokens per wave
-  const int64_t least = 16 * (kRgWaves / m_waves), want = (kCus + p.slices * p.groups - 1) / (p.slices * p.groups);
+  const int64_t least = 16 * (kRgWaves / m_waves), want = (kDwWgs + p.slices * p.groups - 1) / (p.slices * p.groups);
   const int64_t can = (s.T + least - 1) / least;
   int64_t splits = want < can ? want : can;
   if (splits < 1) splits = 1;
@@ -228,31 +230,37 @@ struct RouteGradWs {
   }
 };
 
+template <typename T, int M>
+void launch_route_grad(const RouteGradArgs<T>& a, int wgs, int lds, hipStream_t st) {
+  static std::once_flag configured;
+  std::call_once(configured, [] {
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&route_grad_kernel<T, M>), hipFuncAttributeMaxDynamicSharedMemorySize, kDhLds);
+  });
+  MEFT_LAUNCH("route_grad", (route_grad_kernel<T, M>), dim3((unsigned)wgs), dim3(64 * kRgWaves), lds, st, a);
+}
+
 template <typename T>
 meft_status route_bwd(const meft_shape& s, const void* h, const void* Wg, const float* ds, const void* add, void* dh, void* dWg,
                       float* dbias, void* ws, hipStream_t st) {
   const RouteGradPlan p = route_grad_plan(s);
   const RouteGradWs w(s, ws);
+  const bool dw = dWg || dbias;
+  const int dw_slices = dWg ? p.slices : 1, n_dw = dw ? dw_slices * p.groups * p.splits : 0;
+  // dh: a workgroup for every compute unit beside dWg's, each with at least a tile per wave
+  const int64_t rounds = ((int64_t)s.T + 32 * kRgWaves - 1) / (32 * kRgWaves), most = (kCus + p.slices - 1) / p.slices;
+  const int n_along = (int)(rounds < most ? rounds : most), n_dh = dh ? n_along * p.slices : 0;
+  if (n_dw + n_dh == 0) return MEFT_OK;
   const RouteGradArgs<T> a{static_cast<const T*>(h), static_cast<const T*>(Wg), static_cast<const T*>(add), ds, static_cast<T*>(dh),
-                           static_cast<T*>(dWg), dbias, w.part, w.part_bias, s.T, s.d, s.n_blocks, p.slices, p.m_shift, p.splits,
-                           p.per_split};
-  if (dh && s.T > 0) {
-    static std::once_flag configured;   // up to kDhLds of the router
-    std::call_once(configured, [] {
-      (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&route_dh_kernel<T>), hipFuncAttributeMaxDynamicSharedMemorySize, kDhLds);
-    });
-    const int step = dh_step_bytes<T>(), all = (s.n_blocks + 15) / 16 * step, lds = all < kDhLds ? all : kDhLds;
-    const int64_t rounds = ((int64_t)s.T + 32 * kDhWaves - 1) / (32 * kDhWaves), most = (2 * kCus + p.slices - 1) / p.slices;
-    const dim3 grid((unsigned)(rounds < most ? rounds : most), p.slices);
-    MEFT_LAUNCH("route_dh", route_dh_kernel<T>, grid, dim3(64 * kDhWaves), lds, st, a);
-  }
-  if (dWg || dbias) {
-    const dim3 grid(p.splits, dWg ? p.slices : 1, p.groups);
-    MEFT_LAUNCH("route_dw", route_dw_kernel<T>, grid, dim3(64 * kRgWaves), 0, st, a);
-    if (p.splits > 1) {
-      const int64_t quads = dWg ? (int64_t)s.n_blocks * s.d / 4 : 0;
-      MEFT_LAUNCH("route_dw_join", route_dw_join_kernel<T>, dim3((unsigned)((quads + 255) / 256 + 1)), dim3(256), 0, st, a);
-    }
+                           static_cast<T*>(dWg), dbias, w.part, w.part_bias, s.T, s.d, s.n_blocks, p.m_shift, p.splits,
+                           p.per_split, n_dw, dw_slices, n_along};
+  const int all = dh_steps<T>(s.n_blocks) * dh_step_bytes<T>(), dh_lds = all < kDhLds ? all : kDhLds;
+  const int dw_lds = p.m_shift == 2 ? 4 << 10 : 2 * p.m * 16 << 10;   // two of M * 64 x 64 sums, or the biases
+  const int lds = dh && dh_lds > dw_lds ? dh_lds : dw_lds;
+  if (p.m == 1) launch_route_grad<T, 1>(a, n_dw + n_dh, lds, st);
+  else launch_route_grad<T, 2>(a, n_dw + n_dh, lds, st);
+  if (dw && p.splits > 1) {
+    const int64_t quads = dWg ? (int64_t)s.n_blocks * s.d / 4 : 0;
+    MEFT_LAUNCH("route_dw_join", route_dw_join_kernel<T>, dim3((unsigned)((quads + 255) / 256 + 1)), dim3(256), 0, st, a);
   }
   return launch_status();
 }

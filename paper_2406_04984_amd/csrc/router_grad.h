@@ -28,7 +28,7 @@ struct Rows8<bf16_t> {
   }
   static __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t r, uint32_t at, const float (&v)[4]) {
     const Quad q = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-    __builtin_amdgcn_raw_buffer_store_b64(q, r, (int)at, 0, 2);
+    __builtin_amdgcn_raw_buffer_store_b64(q, r, (int)at, 0, 0);
   }
   // the eight rows of column j
   __device__ __forceinline__ bf16x8 operand(int j) const {
@@ -92,6 +92,7 @@ __device__ __forceinline__ void mma_rows8(const float (&a)[8], const Rows8<float
 __device__ __forceinline__ int tile_row(int r, int lane) { return 8 * (r / 4) + 4 * (lane / 32) + r % 4; }
 
 constexpr int kRgCols = 128;    // columns of a wave's tile
+constexpr int kRgWaves = 4;
 
 template <typename T>
 struct RouteGradArgs {
@@ -100,8 +101,8 @@ struct RouteGradArgs {
   T *dh, *dWg;
   float *dbias, *part, *part_bias;   // part: [split][B][d], where there is more than one split
   int n_tok, d, B;
-  int slices;                        // ceil(d / kRgCols)
   int m_shift, splits, per_split;    // dWg: 2^m_shift waves along the blocks, splits of the tokens, tokens of a split (a multiple of 16)
+  int n_dw, dw_slices, n_along;      // workgroups of dWg, their slices of columns (1 where only dbias is wanted); dh's along the tokens
 };
 
 template <typename T>
@@ -159,31 +160,37 @@ struct StepWords<float> {
   }
 };
 
-constexpr int kDhWaves = 4;
+// steps of ds in registers or on their way: as many as 64 blocks have, half where a step takes eight times as long
+template <typename T>
+constexpr int dh_ahead() { return sizeof(T) == 2 ? 4 : 2; }
+// steps of 16 blocks, rounded up to whole groups of those: what is behind the last block is 0
+template <typename T>
+constexpr int dh_steps(int n_blocks) { return (n_blocks + 16 * dh_ahead<T>() - 1) / (16 * dh_ahead<T>()) * dh_ahead<T>(); }
 constexpr int kDhLds = 128 << 10;   // most of LDS that a workgroup's part of the router takes
 template <typename T>
 constexpr int dh_step_bytes() { return StepWords<T>::kUnits * 64 * 16; }
 
 // dh.  A workgroup holds the router's rows of 128 columns in LDS, as operands, and walks tiles of 32 tokens per wave.  What is
 // added to a tile and its ds are asked for while the tile before is computed.  More blocks than kDhLds holds are staged piece
-// by piece for every tile.  Grid: (workgroups along the tokens, slices): the slices of the same tokens share an XCD's L2, as far as
-// the workgroups along the tokens are a multiple of 8.
-template <typename T>
-__global__ __launch_bounds__(64 * kDhWaves, 2) void route_dh_kernel(RouteGradArgs<T> a) {
+// by piece for every tile.  `along` of `n_along` workgroups along the tokens.  kQuads: the number of
+// blocks is a multiple of 4.  kPieces: they are more
+// than one group of steps.
+template <typename T, bool kQuads, bool kPieces>
+__device__ __forceinline__ void route_dh(const RouteGradArgs<T>& a, int along, int n_along, int slice, u32x4* s_w) {
   typedef Rows8<T> Rows;
   typedef StepWords<T> Words;
-  extern __shared__ u32x4 s_w[];
   constexpr int kMaxSteps = kDhLds / dh_step_bytes<T>();
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c = blockIdx.y * kRgCols + 4 * col;
+  const int c = slice * kRgCols + 4 * col;
   const uint32_t row_bytes = a.d * (uint32_t)sizeof(T), c_bytes = (uint32_t)min(c, a.d - 4) * (uint32_t)sizeof(T);
-  const int steps = (a.B + 15) / 16;
+  constexpr int kAhead = dh_ahead<T>();
+  const int steps = dh_steps<T>(a.B);
   const uint32_t o = 4 * half * row_bytes + (c < a.d ? c_bytes : kNoColumn);
   const uint32_t ds_off = (uint32_t)col * a.B * 4u + 32u * half;
 
   auto stage = [&](int first, int n) {   // steps first .. first + n - 1 of the router
-    for (int s = wave; s < n; s += kDhWaves) {
+    for (int s = wave; s < n; s += kRgWaves) {
       const int b0 = (first + s) * 16;
       const __amdgpu_buffer_rsrc_t wg = rows_at(a.Wg + (size_t)b0 * a.d, min(a.B - b0, 16), row_bytes);
       Rows w;
@@ -195,7 +202,7 @@ __global__ __launch_bounds__(64 * kDhWaves, 2) void route_dh_kernel(RouteGradArg
   // eight values of ds of this lane's token; blocks and tokens that are not there are 0
   auto load_ds = [&](__amdgpu_buffer_rsrc_t ds, int s, u32x4(&x)[2]) {
     const int b = 16 * s + 8 * half;
-    if ((a.B & 3) == 0) {
+    if (kQuads) {
 #pragma unroll
       for (int i = 0; i < 2; ++i)
         x[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ds, (int)(b + 4 * i < a.B ? ds_off + 64 * s + 16 * i : kNoColumn), 0, 0));
@@ -204,57 +211,38 @@ __global__ __launch_bounds__(64 * kDhWaves, 2) void route_dh_kernel(RouteGradArg
       for (int u = 0; u < 8; ++u) x[u / 4][u % 4] = __builtin_amdgcn_raw_buffer_load_b32(ds, (int)(b + u < a.B ? ds_off + 64 * s + 4 * u : kNoColumn), 0, 0);
     }
   };
-  const int64_t tile0 = (int64_t)blockIdx.x * kDhWaves + wave, n_tiles = ((int64_t)a.n_tok + 31) / 32;
-  const int stride = gridDim.x * kDhWaves;
-  auto tile_rows = [&](int64_t tile) { return (int)max((int64_t)0, min((int64_t)32, a.n_tok - tile * 32)); };
+  const int64_t tile0 = (int64_t)along * kRgWaves + wave, n_tiles = ((int64_t)a.n_tok + 31) / 32;
+  const int stride = n_along * kRgWaves;
+  auto tile_rows = [&](int64_t tile) { return tile < 0 ? 0 : (int)max((int64_t)0, min((int64_t)32, a.n_tok - tile * 32)); };
   auto ds_of = [&](int64_t tile) { return rows_at(a.ds + (size_t)tile * 32 * a.B, tile_rows(tile), a.B * 4u); };
 
+  u32x4 x[kAhead][2];
   typename Rows::Quad y[16];   // 0 where nothing is added
   auto load_add = [&](int64_t tile) {
     const __amdgpu_buffer_rsrc_t add = rows_at(a.add + (a.add ? (size_t)tile * 32 * a.d : 0), a.add ? tile_rows(tile) : 0, row_bytes);
 #pragma unroll
     for (int r = 0; r < 16; ++r) y[r] = Rows::load(add, o + (uint32_t)tile_row(r, 0) * row_bytes);
   };
-  constexpr int kAhead = 4;   // steps of ds in registers or on their way
-  u32x4 x[kAhead][2];
-  const int pieces = (steps + kMaxSteps - 1) / kMaxSteps;
-  if (pieces == 1) stage(0, steps);
-  {
-    const __amdgpu_buffer_rsrc_t ds = ds_of(tile0);
+  f32x16 acc[4];
+  // kAhead steps from s0 on, whose router is at `w`; their places in x then take the same steps of another part or tile
+  auto group = [&](const u32x4* w, __amdgpu_buffer_rsrc_t next, int next_s0, bool real = true) {
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) load_ds(ds, i, x[i]);
-  }
-  load_add(tile0);
-  if (pieces == 1) __syncthreads();
-  // every wave of the workgroup makes as many rounds as the first: there may be barriers in them
-  for (int64_t tile = tile0; tile - wave < n_tiles; tile += stride) {
-    const __amdgpu_buffer_rsrc_t ds = ds_of(tile), ds_next = ds_of(tile + stride);
-    f32x16 acc[4];
+    for (int i = 0; i < kAhead; ++i) {
+      float f[8];
+#pragma unroll
+      for (int z = 0; z < 8; ++z) f[z] = __uint_as_float(x[i][z / 4][z % 4]);
+      if (real) Words::mma(f, w + i * Words::kUnits * 64, lane, acc);
+      load_ds(next, next_s0 + i, x[i]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  auto clear = [&] {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[j][r] = 0.f;
-    for (int p = 0; p < pieces; ++p) {
-      const int first = p * kMaxSteps, n = min(steps - first, kMaxSteps);
-      if (pieces > 1) {
-        __syncthreads();
-        stage(first, n);
-        __syncthreads();
-      }
-      for (int s0 = 0; s0 < n; s0 += kAhead) {
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-          float f[8];
-#pragma unroll
-          for (int z = 0; z < 8; ++z) f[z] = __uint_as_float(x[i][z / 4][z % 4]);
-          // the next use of this place: later in the row, or the beginning of the next tile's
-          const int next = first + s0 + i + kAhead;
-          const bool same = first + s0 + kAhead < steps;
-          load_ds(same ? ds : ds_next, same ? next : i, x[i]);
-          if (i == 0 || s0 + i < n) Words::mma(f, s_w + (s0 + i) * Words::kUnits * 64, lane, acc);
-        }
-      }
-    }
+  };
+  auto finish = [&](int64_t tile) {
     const __amdgpu_buffer_rsrc_t to = rows_at(a.dh + (size_t)tile * 32 * a.d, tile_rows(tile), row_bytes);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
@@ -264,53 +252,100 @@ __global__ __launch_bounds__(64 * kDhWaves, 2) void route_dh_kernel(RouteGradArg
       for (int j = 0; j < 4; ++j) v[j] += acc[j][r];
       Rows::store(to, o + (uint32_t)tile_row(r, 0) * row_bytes, v);
     }
+    __builtin_amdgcn_sched_barrier(0);
     load_add(tile + stride);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  if constexpr (kPieces) {
+    const int pieces = (steps + kMaxSteps - 1) / kMaxSteps;
+    if (pieces == 1) stage(0, steps);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) load_ds(ds_of(tile0), i, x[i]);
+    load_add(tile0);
+    if (pieces == 1) __syncthreads();
+    // every wave of the workgroup makes as many rounds as the first: there may be barriers in them
+    for (int64_t tile = tile0; tile - wave < n_tiles; tile += stride) {
+      const __amdgpu_buffer_rsrc_t ds = ds_of(tile), ds_next = ds_of(tile + stride);
+      clear();
+      for (int p = 0; p < pieces; ++p) {
+        const int first = p * kMaxSteps, n = min(steps - first, kMaxSteps);
+        if (pieces > 1) {
+          __syncthreads();
+          stage(first, n);
+          __syncthreads();
+        }
+        for (int s0 = 0; s0 < n; s0 += kAhead) {
+          const bool same = first + s0 + kAhead < steps;
+          group(s_w + s0 * Words::kUnits * 64, same ? ds : ds_next, same ? first + s0 + kAhead : 0);
+        }
+      }
+      finish(tile);
+    }
+  } else {
+    // One round more than there are tiles, the first of a tile before the first one: nothing of it is there, and the loop's
+    // waits for operands are then those of its steady state.
+    stage(0, kAhead);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) x[i][0] = x[i][1] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int r = 0; r < 16; ++r) y[r] = typename Rows::Quad{};
+    for (int64_t tile = tile0 - stride; tile < n_tiles; tile += stride) {
+      clear();
+      group(s_w, ds_of(tile + stride), 0, tile >= tile0);
+      finish(tile);
+    }
   }
 }
 
-constexpr int kRgWaves = 8;
-
-// dWg and dbias.  A wave: 32 blocks x 128 columns over a share of the tokens, 16 at a time, the next step's operands on their
-// way; m_waves waves lie along the blocks, the others share out the tokens and are added through LDS.
-// Grid: (splits, slices, ceil(B / (32 m_waves))), so that the slices of the same tokens share an XCD's L2 (see route_dh_kernel).
-template <typename T>
-__global__ __launch_bounds__(64 * kRgWaves) void route_dw_kernel(RouteGradArgs<T> a) {
+// dWg and dbias.  A wave: 32 M blocks x 128 columns over a share of the tokens, 16 at a time, the next step's operands on their
+// way; 2^m_shift waves lie along the blocks, the others share out the tokens and are added through LDS.
+template <typename T, int M, bool kBias>
+__device__ __forceinline__ void route_dw(const RouteGradArgs<T>& a, int split, int slice, int group, float* lds) {
   typedef Rows8<T> Rows;
-  __shared__ float s_acc[kRgWaves / 2][64][64];
-  __shared__ float s_bias[kRgWaves][32];
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m_waves = 1 << a.m_shift, k_waves = kRgWaves >> a.m_shift, mw = wave & (m_waves - 1), kw = wave >> a.m_shift;
-  const int b0 = ((int)blockIdx.z * m_waves + mw) * 32;
-  const int c = blockIdx.y * kRgCols + 4 * (lane & 31);
-  const int64_t begin = (int64_t)blockIdx.x * a.per_split;
+  const int b0 = (group * m_waves + mw) * 32 * M;
+  const int c = slice * kRgCols + 4 * (lane & 31);
+  const int64_t begin = (int64_t)split * a.per_split;
   const int len = (int)min((int64_t)a.per_split, a.n_tok - begin);   // tokens of this split
   const uint32_t row_bytes = a.d * (uint32_t)sizeof(T), ds_bytes = a.B * 4u;
   const uint32_t h_off = 8 * half * row_bytes + (uint32_t)min(c, a.d - 4) * (uint32_t)sizeof(T);
-  const uint32_t ds_off = 8 * half * ds_bytes + (uint32_t)min(b0 + (lane & 31), a.B - 1) * 4u;
-  f32x16 acc[4];
-  float bias = 0.f;
+  uint32_t ds_off[M];
+  f32x16 acc[M][4];
+  float bias[M];
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
+  for (int m = 0; m < M; ++m) {
+    ds_off[m] = 8 * half * ds_bytes + (uint32_t)min(b0 + 32 * m + (lane & 31), a.B - 1) * 4u;
+    bias[m] = 0.f;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) acc[j][r] = 0.f;
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[m][j][r] = 0.f;
+  }
   constexpr int kAhead = 2;   // steps whose operands are in registers or on their way
   Rows rows[kAhead];
-  float x[kAhead][8];
+  float x[kAhead][M][8];
   const int stride = 16 * k_waves;
-  auto load = [&](int t0, Rows& w, float(&v)[8]) {   // tokens that are not there are 0
+  auto load = [&](int t0, Rows& w, float(&v)[M][8]) {   // tokens that are not there are 0
     const int left = min(len - t0, 16);
     const __amdgpu_buffer_rsrc_t h = rows_at(a.h + (size_t)(begin + t0) * a.d, left, row_bytes);
     const __amdgpu_buffer_rsrc_t ds = rows_at(a.ds + (size_t)(begin + t0) * a.B, left, ds_bytes);
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       w.w[u] = Rows::load(h, h_off + u * row_bytes);
-      v[u] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(ds, (int)(ds_off + u * ds_bytes), 0, 0));
+#pragma unroll
+      for (int m = 0; m < M; ++m)
+        v[m][u] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(ds, (int)(ds_off[m] + u * ds_bytes), 0, 0));
     }
   };
-  auto step = [&](const Rows& w, const float(&v)[8]) {
-    mma_rows8(v, w, acc);
-    bias += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+  auto step = [&](const Rows& w, const float(&v)[M][8]) {
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      mma_rows8(v[m], w, acc[m]);
+      if (kBias) bias[m] += ((v[m][0] + v[m][1]) + (v[m][2] + v[m][3])) + ((v[m][4] + v[m][5]) + (v[m][6] + v[m][7]));
+    }
   };
 #pragma unroll
   for (int i = 0; i < kAhead - 1; ++i) load(16 * kw + i * stride, rows[i], x[i]);
@@ -318,51 +353,91 @@ __global__ __launch_bounds__(64 * kRgWaves) void route_dw_kernel(RouteGradArgs<T
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       load(t0 + (i + kAhead - 1) * stride, rows[(i + kAhead - 1) % kAhead], x[(i + kAhead - 1) % kAhead]);
-      if (i == 0 || t0 + i * stride < len) step(rows[i], x[i]);
+      __builtin_amdgcn_sched_barrier(0);   // the compiler would ask for a step's operands at the end of the step before
+      step(rows[i], x[i]);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
   // the waves that shared out the tokens, in pairs
   for (int n = k_waves / 2; n > 0; n /= 2) {
     __syncthreads();
-    float(*s)[64] = s_acc[(kw & (n - 1)) * m_waves + mw];
+    float* s = lds + ((kw & (n - 1)) * m_waves + mw) * (M * 64 * 64) + lane;
     if (kw >= n && kw < 2 * n) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int m = 0; m < M; ++m)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[j * 16 + r][lane] = acc[j][r];
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[((m * 4 + j) * 16 + r) * 64] = acc[m][j][r];
     }
     __syncthreads();
     if (kw < n) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int m = 0; m < M; ++m)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[j][r] += s[j * 16 + r][lane];
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[m][j][r] += s[((m * 4 + j) * 16 + r) * 64];
     }
   }
-  if (blockIdx.y == 0) {
-    bias += __shfl_xor(bias, 32, kWave);
-    if (half == 0) s_bias[wave][lane] = bias;
+  if (kBias) {
     __syncthreads();
-    if (kw == 0 && half == 0 && a.dbias) {
-      float v = 0.f;
-      for (int k = 0; k < k_waves; ++k) v += s_bias[k * m_waves + mw][lane];
-      if (b0 + lane < a.B) (a.splits > 1 ? a.part_bias + (size_t)blockIdx.x * a.B : a.dbias)[b0 + lane] = v;
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      const float v = bias[m] + __shfl_xor(bias[m], 32, kWave);
+      if (half == 0) lds[(wave * M + m) * 32 + lane] = v;
+    }
+    __syncthreads();
+    if (kw == 0 && half == 0) {
+#pragma unroll
+      for (int m = 0; m < M; ++m) {
+        const int b = b0 + 32 * m + lane;
+        float v = 0.f;
+        for (int k = 0; k < k_waves; ++k) v += lds[((k * m_waves + mw) * M + m) * 32 + lane];
+        if (b < a.B) (a.splits > 1 ? a.part_bias + (size_t)split * a.B : a.dbias)[b] = v;
+      }
     }
   }
   if (kw != 0 || !a.dWg) return;
-  const int left = min(a.B - b0, 32);
-  if (a.splits > 1) {
-    const __amdgpu_buffer_rsrc_t to = rows_at(a.part + ((size_t)blockIdx.x * a.B + b0) * a.d, left, a.d * 4u);
-    const uint32_t o = 4 * half * a.d * 4u + (c < a.d ? c * 4u : kNoColumn);
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
-      Rows8<float>::store(to, o + (uint32_t)tile_row(r, 0) * a.d * 4u, {acc[0][r], acc[1][r], acc[2][r], acc[3][r]});
+  for (int m = 0; m < M; ++m) {
+    const int first = b0 + 32 * m, left = min(a.B - first, 32);
+    if (a.splits > 1) {
+      const __amdgpu_buffer_rsrc_t to = rows_at(a.part + ((size_t)split * a.B + first) * a.d, left, a.d * 4u);
+      const uint32_t o = 4 * half * a.d * 4u + (c < a.d ? c * 4u : kNoColumn);
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        Rows8<float>::store(to, o + (uint32_t)tile_row(r, 0) * a.d * 4u, {acc[m][0][r], acc[m][1][r], acc[m][2][r], acc[m][3][r]});
+    } else {
+      const __amdgpu_buffer_rsrc_t to = rows_at(a.dWg + (size_t)first * a.d, left, row_bytes);
+      const uint32_t o = 4 * half * row_bytes + (c < a.d ? c * (uint32_t)sizeof(T) : kNoColumn);
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        Rows::store(to, o + (uint32_t)tile_row(r, 0) * row_bytes, {acc[m][0][r], acc[m][1][r], acc[m][2][r], acc[m][3][r]});
+    }
+  }
+}
+
+// Both in one launch, so that neither's start and end leave the memory idle: the first n_dw workgroups compute dWg, the others dh.
+// Along the tokens fastest, so that the slices of the same tokens share an XCD's L2.
+template <typename T, int M>
+__global__ __launch_bounds__(64 * kRgWaves, 2) void route_grad_kernel(RouteGradArgs<T> a) {
+  extern __shared__ u32x4 s_lds[];
+  const int id = blockIdx.x;
+  if (id < a.n_dw) {
+    const int rest = __builtin_amdgcn_readfirstlane(id / a.splits), group = __builtin_amdgcn_readfirstlane(rest / a.dw_slices);
+    const int split = id - rest * a.splits, slice = rest - group * a.dw_slices;
+    if (slice == 0 && a.dbias) route_dw<T, M, true>(a, split, slice, group, reinterpret_cast<float*>(s_lds));
+    else route_dw<T, M, false>(a, split, slice, group, reinterpret_cast<float*>(s_lds));
   } else {
-    const __amdgpu_buffer_rsrc_t to = rows_at(a.dWg + (size_t)b0 * a.d, left, row_bytes);
-    const uint32_t o = 4 * half * row_bytes + (c < a.d ? c * (uint32_t)sizeof(T) : kNoColumn);
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-      Rows::store(to, o + (uint32_t)tile_row(r, 0) * row_bytes, {acc[0][r], acc[1][r], acc[2][r], acc[3][r]});
+    const int i = id - a.n_dw, slice = __builtin_amdgcn_readfirstlane(i / a.n_along), along = i - slice * a.n_along;
+    if (dh_steps<T>(a.B) == dh_ahead<T>()) {
+      if (a.B % 4 == 0) route_dh<T, true, false>(a, along, a.n_along, slice, s_lds);
+      else route_dh<T, false, false>(a, along, a.n_along, slice, s_lds);
+    } else {
+      if (a.B % 4 == 0) route_dh<T, true, true>(a, along, a.n_along, slice, s_lds);
+      else route_dh<T, false, true>(a, along, a.n_along, slice, s_lds);
+    }
   }
 }
 
