@@ -29,30 +29,39 @@ NormShape norm_shape(int d) {
   if (groups <= 64) return {1, 1};
   if (groups <= 128) return {2, 1};
   if (groups <= 256) return {1, 4};
-  if (groups <= 512) return {2, 4};
+  if (groups <= 512) return {1, 8};
   if (groups <= 1024) return {2, 8};
   return {2, 16};
 }
 
-constexpr int kNormBwdWgs = 512;
-int norm_bwd_slots(int w) { return w > 8 ? 1 : 8 / w; }
-// workgroups of the backward, each of which leaves partial sums of dgamma and dbeta
-int norm_bwd_grid(const meft_shape& s) {
-  const int slots = norm_bwd_slots(norm_shape(s.d).w);
-  const int64_t need = ((int64_t)s.T + slots - 1) / slots;
-  return (int)(need < 1 ? 1 : need < kNormBwdWgs ? need : kNormBwdWgs);
+// Rows of a workgroup: as many as leave every compute unit a workgroup.
+int norm_slots(const meft_shape& s) {
+  int slots = norm_max_slots(norm_shape(s.d).w);
+  while (slots > 1 && (s.T + slots - 1) / slots < kCus) slots /= 2;
+  return slots;
 }
+int norm_grid(const meft_shape& s, int most) {
+  const int slots = norm_slots(s);
+  const int64_t need = ((int64_t)s.T + slots - 1) / slots;
+  return (int)(need < 1 ? 1 : need < most ? need : most);
+}
+// Workgroups of the backward, each of which leaves partial sums of dgamma and dbeta: at least eight rows for each slot before a
+// compute unit gets a second workgroup (layer kind with dropout, d 4096, us, 256 / 512 of them: 2003 tokens 18.7 / 20.2, 8192
+// tokens 63 / 60).
+int norm_bwd_grid(const meft_shape& s) {
+  const int64_t eight = (int64_t)s.T / (8 * norm_slots(s));
+  return norm_grid(s, eight < kCus ? kCus : eight < 2 * kCus ? (int)eight : 2 * kCus);
+}
+int norm_fwd_grid(const meft_shape& s) { return norm_grid(s, 8 * kCus); }
 
-#define MEFT_NORM_SHAPES(X) X(1, 1) X(2, 1) X(1, 4) X(2, 4) X(2, 8) X(2, 16)
+#define MEFT_NORM_SHAPES(X) X(1, 1) X(2, 1) X(1, 4) X(1, 8) X(2, 8) X(2, 16)
 
 template <typename T, int kMode>
 void launch_norm_fwd(const meft_shape& s, const NormFwdArgs<T>& a, hipStream_t st) {
   const NormShape n = norm_shape(s.d);
-  const int slots = n.w > 4 ? 1 : 4 / n.w, threads = n.w > 4 ? 64 * n.w : 256;
-  const int64_t need = ((int64_t)s.T + slots - 1) / slots, most = (int64_t)kCus * (2048 / threads);
-  const dim3 grid((unsigned)(need < most ? need : most));
+  const dim3 grid(norm_fwd_grid(s)), block(64 * n.w * norm_slots(s));
 #define X(V, W) \
-  if (n.v == V && n.w == W) MEFT_LAUNCH("norm_fwd", (norm_fwd_kernel<T, V, W, kMode>), grid, dim3(threads), 0, st, a);
+  if (n.v == V && n.w == W) MEFT_LAUNCH("norm_fwd", (norm_fwd_kernel<T, V, W, kMode>), grid, block, 0, st, a);
   MEFT_NORM_SHAPES(X)
 #undef X
 }
@@ -60,7 +69,7 @@ void launch_norm_fwd(const meft_shape& s, const NormFwdArgs<T>& a, hipStream_t s
 template <typename T, int kMode, int kGrads>
 void launch_norm_bwd(const meft_shape& s, const NormBwdArgs<T>& a, hipStream_t st) {
   const NormShape n = norm_shape(s.d);
-  const dim3 grid(norm_bwd_grid(s)), block(n.w > 8 ? 64 * n.w : 512);
+  const dim3 grid(norm_bwd_grid(s)), block(64 * n.w * norm_slots(s));
 #define X(V, W) \
   if (n.v == V && n.w == W) MEFT_LAUNCH("norm_bwd", (norm_bwd_kernel<T, V, W, kMode, kGrads>), grid, block, 0, st, a);
   MEFT_NORM_SHAPES(X)
@@ -135,7 +144,7 @@ meft_status norm_bwd(const meft_shape& s, const meft_norm& n, int mode, const Dr
   else if (mode == kNormAdd) norm_bwd_grads<T, kNormAdd>(s, a, grads, st);
   else norm_bwd_grads<T, kNormDrop>(s, a, grads, st);
   if (grads)
-    MEFT_LAUNCH("norm_grad", norm_grad_kernel<T>, dim3((s.d + 63) / 64, grads), dim3(256), 0, st, w.part, norm_bwd_grid(s), s.d,
+    MEFT_LAUNCH("norm_grad", norm_grad_kernel<T>, dim3((s.d + 31) / 32, grads), dim3(512), 0, st, w.part, norm_bwd_grid(s), s.d,
                 static_cast<T*>(dgamma), static_cast<T*>(dbeta));
   return launch_status();
 }

@@ -120,6 +120,22 @@ struct Vec16<bf16_t> {
   static __device__ __forceinline__ void store_f32(float* p, const float (&v)[8]) { Vec8<float>::store(p, v); }
 };
 
+// p[0] + p[step] + ... of n places, in that order, eight on their way at a time: one after the other, a handful of places takes
+// as many round trips to memory (0.5 to 1 us each)
+template <typename V>
+__device__ __forceinline__ V sum_places(const V* p, int n, size_t step) {
+  V sum{};
+  for (int i = 0; i < n; i += 8) {
+    V v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = p[(size_t)min(i + u, n - 1) * step];
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (i + u < n) sum += v[u];
+  }
+  return sum;
+}
+
 // ---- wave-level reductions -----------------------------------------------------------------
 // sum over the wave, in every lane: DPP moves inside the rows of 16 lanes, then two lane permutes
 __device__ __forceinline__ float wave_sum(float v) {

@@ -24,6 +24,11 @@ struct Raw8 {
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(T) / 2); ++i) w[i] = u32x4{0u, 0u, 0u, 0u};
   }
+  // what was widened from the words is not kept beyond here: it is widened from them again
+  __device__ __forceinline__ void forget() {
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) asm volatile("" : "+v"(w[i]));
+  }
   __device__ __forceinline__ void widen(float (&v)[8]) const {
     if constexpr (sizeof(T) == 2) {
       Vec8<bf16_t>::widen(w[0], v);
@@ -49,15 +54,15 @@ __device__ __forceinline__ void round8(float (&v)[8]) {
 
 // Sums over the W waves of a row.  Calls alternate between two buffers, so one barrier each is enough: a wave writes a buffer
 // again only behind the barrier of the call in between, which the last reader of the former contents has passed.
-template <int W, int kSlots, int kValues>
+template <int W, int kMaxSlots, int kValues>
 struct RowSum {
-  float* lds;   // [2][kSlots][W][kValues]
+  float* lds;   // [2][kMaxSlots][W][kValues]
   int turn = 0;
   __device__ __forceinline__ void operator()(float (&v)[kValues], int slot, int wave) {
 #pragma unroll
     for (int i = 0; i < kValues; ++i) v[i] = wave_sum(v[i]);
     if constexpr (W > 1) {
-      float* p = lds + (size_t)((turn * kSlots + slot) * W) * kValues;
+      float* p = lds + (size_t)((turn * kMaxSlots + slot) * W) * kValues;
       turn ^= 1;
       if ((threadIdx.x & 63) < kValues) {
         float mine = v[0];
@@ -89,14 +94,19 @@ struct NormFwdArgs {
   DropArgs drop;
 };
 
+// Rows (slots of W waves) of a workgroup of norm_fwd_kernel and norm_bwd_kernel at most; the launch says how many there are.
+constexpr int norm_max_slots(int w) { return w >= 4 ? 1 : 4 / w; }
+
+// A row's words are asked for while the row before is computed: they are widened at the top of a round, and their registers
+// then take the next row's.
 template <typename T, int V, int W, int kMode>
-__global__ __launch_bounds__(W > 4 ? 64 * W : 256) void norm_fwd_kernel(NormFwdArgs<T> a) {
-  constexpr int kSlots = W > 4 ? 1 : 4 / W;
-  __shared__ float s_sum[2 * kSlots * W];
-  const int slot = threadIdx.x / (64 * W), q = threadIdx.x % (64 * W), wave = q / 64;
-  RowSum<W, kSlots, 1> row_sum{s_sum};
+__global__ __launch_bounds__(64 * W * norm_max_slots(W)) void norm_fwd_kernel(NormFwdArgs<T> a) {
+  constexpr int kMaxSlots = norm_max_slots(W);
+  __shared__ float s_sum[2 * kMaxSlots * W];
+  const int slots = blockDim.x / (64 * W), slot = threadIdx.x / (64 * W), q = threadIdx.x % (64 * W), wave = q / 64;
+  RowSum<W, kMaxSlots, 1> row_sum{s_sum};
   const uint64_t offset = kMode == kNormDrop ? drop_offset(a.drop) : 0;
-  Raw8<T> gamma[V], beta[V];
+  Raw8<T> gamma[V], beta[V], raw_x[V], raw_out[V];
   bool in[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
@@ -104,29 +114,44 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void norm_fwd_kernel(NormFwdA
     in[i] = c < a.d;
     gamma[i].clear();
     beta[i].clear();
+    raw_x[i].clear();
+    raw_out[i].clear();
     if (in[i]) gamma[i].load(a.gamma + c);
     if (in[i] && a.beta) beta[i].load(a.beta + c);
   }
-  for (int64_t first = (int64_t)blockIdx.x * kSlots; first < a.n_tok; first += (int64_t)gridDim.x * kSlots) {
-    const int64_t t = first + slot;
-    const bool live = t < a.n_tok;
+  auto load = [&](int64_t t) {
+    if (t >= a.n_tok) return;
     const size_t row = (size_t)t * a.d;
-    float v[V][8];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int c = (i * 64 * W + q) * 8;
+      if (!in[i]) continue;
+      raw_x[i].load(a.x + row + c);
+      if (kMode != kNormPlain) raw_out[i].load(a.out + row + c);
+    }
+  };
+  const int64_t stride = (int64_t)gridDim.x * slots;
+  load((int64_t)blockIdx.x * slots + slot);
+  for (int64_t first = (int64_t)blockIdx.x * slots; first < a.n_tok; first += stride) {
+    const int64_t t = first + slot;
+    const bool live = t < a.n_tok;
+    const size_t row = (size_t)t * a.d;
+    float v[V][8], o[V][8];
 #pragma unroll
-      for (int z = 0; z < 8; ++z) v[i][z] = 0.f;
-      if (!live || !in[i]) continue;
-      Vec8<T>::load(a.x + row + c, v[i]);
-      if (kMode != kNormPlain) {
-        float o[8];
-        Vec8<T>::load(a.out + row + c, o);
-        if (kMode == kNormDrop) drop8(a.drop, offset, (uint32_t)t, c / 8, o);
+    for (int i = 0; i < V; ++i) {
+      raw_x[i].widen(v[i]);
+      if (kMode != kNormPlain) raw_out[i].widen(o[i]);
+    }
+    load(t + stride);
+    if (kMode != kNormPlain) {
 #pragma unroll
-        for (int z = 0; z < 8; ++z) v[i][z] += o[z];
+      for (int i = 0; i < V; ++i) {
+        const int c = (i * 64 * W + q) * 8;
+        if (kMode == kNormDrop) drop8(a.drop, offset, (uint32_t)t, c / 8, o[i]);
+#pragma unroll
+        for (int z = 0; z < 8; ++z) v[i][z] += o[i][z];
         round8<T>(v[i]);   // the norm is of the stream as it is stored, which is what the backward reads
-        Vec8<T>::store(a.y + row + c, v[i]);
+        if (live && in[i]) Vec8<T>::store(a.y + row + c, v[i]);
       }
     }
     float mean[1] = {0.f}, sq[1] = {0.f};
@@ -179,49 +204,97 @@ struct NormBwdArgs {
 // kGrads: 0 dx only, 1 and dgamma, 2 and dbeta.  A workgroup walks rows with the weight's gradient of its columns in
 // registers; the slots of a workgroup are added through LDS, the workgroups by norm_grad_kernel, both in a fixed order.
 template <typename T, int V, int W, int kMode, int kGrads>
-__global__ __launch_bounds__(W > 8 ? 64 * W : 512) void norm_bwd_kernel(NormBwdArgs<T> a) {
-  constexpr int kSlots = W > 8 ? 1 : 8 / W;
-  __shared__ float s_sum[2 * kSlots * W * 2];
-  __shared__ __attribute__((aligned(16))) float s_acc[kGrads && kSlots > 1 ? 64 * W * V * 8 : 4];
-  const int slot = threadIdx.x / (64 * W), q = threadIdx.x % (64 * W), wave = q / 64;
-  RowSum<W, kSlots, 2> row_sum{s_sum};
+__global__ __launch_bounds__(64 * W * norm_max_slots(W)) void norm_bwd_kernel(NormBwdArgs<T> a) {
+  constexpr int kMaxSlots = norm_max_slots(W);
+  __shared__ float s_sum[2 * kMaxSlots * W * 2];
+  __shared__ __attribute__((aligned(16))) float s_acc[kGrads && kMaxSlots > 1 ? 64 * W * V * 8 : 4];
+  const int slots = blockDim.x / (64 * W), slot = threadIdx.x / (64 * W), q = threadIdx.x % (64 * W), wave = q / 64;
+  RowSum<W, kMaxSlots, 2> row_sum{s_sum};
   const uint64_t offset = kMode == kNormDrop ? drop_offset(a.drop) : 0;
-  Raw8<T> gamma[V];
-  float dgamma[V][8], dbeta[V][8];
+  Raw8<T> gamma[V], raw_y[V], raw_dh[V], raw_dy[V];
+  float dgamma[V][8], dbeta[V][8], rstd_next = 0.f, mean_next = 0.f;
   bool in[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const int c = (i * 64 * W + q) * 8;
     in[i] = c < a.d;
     gamma[i].clear();
+    raw_y[i].clear();
+    raw_dh[i].clear();
+    raw_dy[i].clear();
     if (in[i]) gamma[i].load(a.gamma + c);
 #pragma unroll
     for (int z = 0; z < 8; ++z) dgamma[i][z] = dbeta[i][z] = 0.f;
   }
-  for (int64_t first = (int64_t)blockIdx.x * kSlots; first < a.n_tok; first += (int64_t)gridDim.x * kSlots) {
-    const int64_t t = first + slot;
-    const bool live = t < a.n_tok;
+  auto load = [&](int64_t t) {
+    if (t >= a.n_tok) return;
     const size_t row = (size_t)t * a.d;
-    const float rstd = live ? a.rstd[t] : 0.f, mean = live && a.layer ? a.mean[t] : 0.f;
-    float g[V][8], xh[V][8], s[2] = {0.f, 0.f};
+    rstd_next = a.rstd[t];
+    if (a.layer) mean_next = a.mean[t];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int c = (i * 64 * W + q) * 8;
+      if (!in[i]) continue;
+      raw_y[i].load(a.y + row + c);
+      raw_dh[i].load(a.dh + row + c);
+      if (a.dy) raw_dy[i].load(a.dy + row + c);
+    }
+  };
+  const int64_t stride = (int64_t)gridDim.x * slots;
+  constexpr bool kAhead = W < 16;   // 1024 threads have 128 registers each: none for a row to come
+  if (kAhead) load((int64_t)blockIdx.x * slots + slot);
+  for (int64_t first = (int64_t)blockIdx.x * slots; first < a.n_tok; first += stride) {
+    const int64_t t = first + slot;
+    if (!kAhead) load(t);
+    const bool live = t < a.n_tok;   // a slot behind the last row computes on a row of before and keeps nothing
+    const size_t row = (size_t)t * a.d;
+    const float rstd = rstd_next, mean = mean_next;
+    // the row's values in fp32 where their words make room for the next row's, else widened again behind the sums
+    constexpr int kHeld = kAhead ? V : 1;
+    float g[kHeld][8], xh[kHeld][8], r[kHeld][8], s[2] = {0.f, 0.f};
+    auto widen = [&](int i, float(&x8)[8], float(&g8)[8]) {
+      raw_y[i].widen(x8);
+      raw_dh[i].widen(g8);
 #pragma unroll
-      for (int z = 0; z < 8; ++z) g[i][z] = xh[i][z] = 0.f;
-      if (!live || !in[i]) continue;
-      Vec8<T>::load(a.y + row + c, xh[i]);
-      Vec8<T>::load(a.dh + row + c, g[i]);
+      for (int z = 0; z < 8; ++z) x8[z] = in[i] ? (x8[z] - mean) * rstd : 0.f;
+    };
+    auto weigh = [&](int i, float(&g8)[8]) {
       float gm[8];
       gamma[i].widen(gm);
 #pragma unroll
+      for (int z = 0; z < 8; ++z) g8[z] *= gm[z];
+    };
+    auto sums = [&](int i, float(&x8)[8], float(&g8)[8]) {
+#pragma unroll
       for (int z = 0; z < 8; ++z) {
-        xh[i][z] = (xh[i][z] - mean) * rstd;
-        if (kGrads > 0) dgamma[i][z] += g[i][z] * xh[i][z];
-        if (kGrads > 1) dbeta[i][z] += g[i][z];
-        g[i][z] *= gm[z];
-        s[0] += g[i][z];
-        s[1] += g[i][z] * xh[i][z];
+        if (kGrads > 0) dgamma[i][z] += live ? g8[z] * x8[z] : 0.f;
+        if (kGrads > 1) dbeta[i][z] += live ? g8[z] : 0.f;
+      }
+      weigh(i, g8);
+#pragma unroll
+      for (int z = 0; z < 8; ++z) {
+        s[0] += g8[z];
+        s[1] += g8[z] * x8[z];
+      }
+    };
+    if constexpr (kAhead) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        widen(i, xh[i], g[i]);
+        raw_dy[i].widen(r[i]);
+      }
+      load(t + stride);
+#pragma unroll
+      for (int i = 0; i < V; ++i) sums(i, xh[i], g[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        widen(i, xh[0], g[0]);
+        sums(i, xh[0], g[0]);
+        raw_y[i].forget();
+        raw_dh[i].forget();
+        raw_dy[i].forget();
+        gamma[i].forget();
       }
     }
     row_sum(s, slot, wave);
@@ -230,19 +303,19 @@ __global__ __launch_bounds__(W > 8 ? 64 * W : 512) void norm_bwd_kernel(NormBwdA
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       if (!in[i]) continue;
-      const int c = (i * 64 * W + q) * 8;
-      float r[8];
-#pragma unroll
-      for (int z = 0; z < 8; ++z) g[i][z] = rstd * (g[i][z] - m0 - xh[i][z] * m1);
-      if (a.dy) {
-        Vec8<T>::load(a.dy + row + c, r);
-#pragma unroll
-        for (int z = 0; z < 8; ++z) g[i][z] += r[z];
+      constexpr bool held = kAhead;
+      const int c = (i * 64 * W + q) * 8, k = held ? i : 0;
+      if (!held) {
+        widen(i, xh[k], g[k]);
+        weigh(i, g[k]);
+        raw_dy[i].widen(r[k]);
       }
-      Vec8<T>::store(a.dx + row + c, g[i]);
+#pragma unroll
+      for (int z = 0; z < 8; ++z) g[k][z] = rstd * (g[k][z] - m0 - xh[k][z] * m1) + r[k][z];
+      Vec8<T>::store(a.dx + row + c, g[k]);
       if (kMode != kNormPlain) {
-        if (kMode == kNormDrop) drop8(a.drop, offset, (uint32_t)t, c / 8, g[i]);
-        Vec8<T>::store(a.dout + row + c, g[i]);
+        if (kMode == kNormDrop) drop8(a.drop, offset, (uint32_t)t, c / 8, g[k]);
+        Vec8<T>::store(a.dout + row + c, g[k]);
       }
     }
   }
@@ -251,8 +324,8 @@ __global__ __launch_bounds__(W > 8 ? 64 * W : 512) void norm_bwd_kernel(NormBwdA
 #pragma unroll
     for (int which = 0; which < kGrads; ++which) {
       float(&acc)[V][8] = which == 0 ? dgamma : dbeta;
-      if constexpr (kSlots > 1) {
-        for (int other = 1; other < kSlots; ++other) {
+      if constexpr (kMaxSlots > 1) {
+        for (int other = 1; other < slots; ++other) {
           __syncthreads();
           if (slot == other)
 #pragma unroll
@@ -276,25 +349,28 @@ __global__ __launch_bounds__(W > 8 ? 64 * W : 512) void norm_bwd_kernel(NormBwdA
   }
 }
 
-// dgamma and dbeta (blockIdx.y) from the workgroups' partial sums: 16 threads along 64 columns, 16 along the workgroups
+// dgamma and dbeta (blockIdx.y) from the workgroups' partial sums: 8 threads along 32 columns, 64 along the workgroups
 template <typename T>
-__global__ __launch_bounds__(256) void norm_grad_kernel(const float* __restrict__ part, int n_part, int d, T* dgamma, T* dbeta) {
-  __shared__ __attribute__((aligned(16))) float s[16][64];
-  const int q = threadIdx.x & 15, g = threadIdx.x >> 4, c = blockIdx.x * 64 + q * 4;
-  const float* p = part + (size_t)blockIdx.y * d;
+__global__ __launch_bounds__(512) void norm_grad_kernel(const float* __restrict__ part, int n_part, int d, T* dgamma, T* dbeta) {
+  __shared__ __attribute__((aligned(16))) float s[64][32];
+  const int q = threadIdx.x & 7, g = threadIdx.x >> 3, c = blockIdx.x * 32 + q * 4;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  if (c < d)
-    for (int i = g; i < n_part; i += 16) v += *reinterpret_cast<const f32x4*>(p + (size_t)i * 2 * d + c);
+  if (c < d && g < n_part)
+    v = sum_places(reinterpret_cast<const f32x4*>(part + ((size_t)g * 2 + blockIdx.y) * d + c), (n_part - g + 63) / 64, (size_t)32 * d);
   *reinterpret_cast<f32x4*>(&s[g][q * 4]) = v;
   __syncthreads();
-  const int col = blockIdx.x * 64 + threadIdx.x;
-  if (threadIdx.x < 64 && col < d) {
+  if (threadIdx.x < 256) {   // eight threads a column
+    const int lc = threadIdx.x >> 3, k = threadIdx.x & 7, col = blockIdx.x * 32 + lc;
     float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sum += s[i][threadIdx.x];
-    T* o = blockIdx.y == 0 ? dgamma : dbeta;
-    if constexpr (sizeof(T) == 2) o[col].bits = (uint16_t)pack_bf16x2(sum, 0.f);
-    else o[col] = sum;
+    for (int i = 0; i < 8; ++i) sum += s[k * 8 + i][lc];
+#pragma unroll
+    for (int o = 1; o < 8; o *= 2) sum += __shfl_xor(sum, o, kWave);
+    if (k == 0 && col < d) {
+      T* out = blockIdx.y == 0 ? dgamma : dbeta;
+      if constexpr (sizeof(T) == 2) out[col].bits = (uint16_t)pack_bf16x2(sum, 0.f);
+      else out[col] = sum;
+    }
   }
 }
 

@@ -446,19 +446,10 @@ template <typename T>
 __global__ __launch_bounds__(256) void route_dw_join_kernel(RouteGradArgs<T> a) {
   const int64_t n = (int64_t)a.B * a.d, i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
   if (a.dbias && blockIdx.x == gridDim.x - 1)
-    for (int b = threadIdx.x; b < a.B; b += 256) {
-      float v = 0.f;
-      for (int s = 0; s < a.splits; ++s) v += a.part_bias[(size_t)s * a.B + b];
-      a.dbias[b] = v;
-    }
+    for (int b = threadIdx.x; b < a.B; b += 256) a.dbias[b] = sum_places(a.part_bias + b, a.splits, a.B);
   if (i >= n || !a.dWg) return;
-  float v[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < a.splits; ++s) {
-    const f32x4 x = *reinterpret_cast<const f32x4*>(a.part + (size_t)s * n + i);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] += x[j];
-  }
-  store4(a.dWg + i, v);
+  const f32x4 v = sum_places(reinterpret_cast<const f32x4*>(a.part + i), a.splits, (size_t)(n / 4));
+  store4(a.dWg + i, {v[0], v[1], v[2], v[3]});
 }
 
 }  // namespace meft
