@@ -149,11 +149,13 @@ meft_status norm_bwd(const meft_shape& s, const meft_norm& n, int mode, const Dr
   return launch_status();
 }
 
+constexpr int kDropWgs = 8 * kCus;   // workgroups of dropout_add at most
+
 // ---- balance --------------------------------------------------------------------------------
-// waves of a row of scores
+// waves of a row of scores, and the scores of a lane
 int balance_waves(const meft_shape& s) { return s.n_blocks <= 1024 ? 1 : 16; }
 int balance_grid(const meft_shape& s) {
-  const int rows = balance_waves(s) == 1 ? 4 : 1;
+  const int rows = balance_rows(balance_waves(s), s.n_blocks <= 256 ? 4 : 16);
   const int64_t need = ((int64_t)s.T + rows - 1) / rows;
   return (int)(need < 1 ? 1 : need < kCus ? need : kCus);
 }
@@ -188,7 +190,8 @@ static_assert(kMaxBlocks <= 16 * 16 * 64, "balance_part_kernel and balance_grad_
 template <int Z, int W>
 void launch_balance_part(const meft_shape& s, const float* scores, const int32_t* block_idx, const uint8_t* valid,
                          const BalancePart& part, hipStream_t st) {
-  const size_t lds = (size_t)s.n_blocks * 4 * (W == 1 ? 5 : 1);
+  constexpr int rows = balance_rows(W, Z);
+  const size_t lds = (size_t)s.n_blocks * 4 * (W == 1 ? rows + 1 : 1);
   if (W > 1) {
     static std::once_flag configured;   // up to 64 KB of counts beside the waves' values
     std::call_once(configured, [] {
@@ -196,7 +199,7 @@ void launch_balance_part(const meft_shape& s, const float* scores, const int32_t
                                 kMaxBlocks * 4);
     });
   }
-  MEFT_LAUNCH("balance_part", (balance_part_kernel<Z, W>), dim3(balance_grid(s)), dim3(W == 1 ? 256 : 64 * W), lds, st, scores,
+  MEFT_LAUNCH("balance_part", (balance_part_kernel<Z, W>), dim3(balance_grid(s)), dim3(balance_threads<Z, W>()), lds, st, scores,
               block_idx, valid, s.T, s.n_blocks, s.top_e, part);
 }
 
@@ -340,14 +343,17 @@ meft_status meft_dropout_add(const meft_shape* shape, const meft_drop* drop, con
   if (thr < 0 || !aligned_as<uint64_t>(step) || !ok16(out) || !null_or16(res) || !ok16(y)) return MEFT_ERR_INVALID_ARG;
   if (s.T == 0) return MEFT_OK;
   const int groups = s.d / 8;
-  const int64_t wgs = ((int64_t)s.T * groups + 256 * kDropGroups - 1) / (256 * kDropGroups), x = wgs < (1 << 23) ? wgs : 1 << 23;
-  const dim3 grid((unsigned)x, (unsigned)((wgs + x - 1) / x));   // a launch takes fewer than 2^32 threads along x
+  const int64_t spans = ((int64_t)s.T * groups + kDropSpan - 1) / kDropSpan, most = kDropWgs;
+  const int64_t wgs = spans < most ? spans : most;
+  const dim3 grid((unsigned)wgs);
+  const uint32_t step_t = (uint32_t)(wgs * kDropSpan / groups), step_g = (uint32_t)(wgs * kDropSpan % groups);
   hipStream_t st = static_cast<hipStream_t>(stream);
   const DropArgs a = drop_args(drop, step, thr);
   MEFT_API_LOCK();
   clear_stale_error();
 #define DROPOUT(TY, DROP) MEFT_LAUNCH("dropout_add", (dropout_add_kernel<TY, DROP>), grid, dim3(256), 0, st, static_cast<const TY*>(out), \
-                                     static_cast<const TY*>(res), static_cast<TY*>(y), s.T, groups, tile_div_inverse(groups), a)
+                                     static_cast<const TY*>(res), static_cast<TY*>(y), s.T, groups, tile_div_inverse(groups), \
+                                     step_t, step_g, a)
   if (s.dtype == MEFT_BF16) {
     if (thr) DROPOUT(bf16_t, true);
     else DROPOUT(bf16_t, false);

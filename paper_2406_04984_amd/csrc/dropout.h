@@ -42,39 +42,85 @@ __device__ __forceinline__ void drop8(const DropArgs& a, uint64_t offset, uint32
   }
 }
 
-constexpr int kDropGroups = 4;   // groups of eight columns per thread
+template <typename T>
+struct Raw8 {
+  u32x4 w[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) w[i] = reinterpret_cast<const u32x4*>(p)[i];
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) w[i] = u32x4{0u, 0u, 0u, 0u};
+  }
+  // what was widened from the words is not kept beyond here: it is widened from them again
+  __device__ __forceinline__ void forget() {
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) asm volatile("" : "+v"(w[i]));
+  }
+  __device__ __forceinline__ void widen(float (&v)[8]) const {
+    if constexpr (sizeof(T) == 2) {
+      Vec8<bf16_t>::widen(w[0], v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i / 4][i % 4]);
+    }
+  }
+};
 
-// One workgroup takes 256 * kDropGroups consecutive groups.  y may be out or res: a thread reads its elements before it
-// writes them.
+constexpr int kDropGroups = 2;                    // groups of eight columns per thread and round
+constexpr int kDropSpan = 256 * kDropGroups;      // of a workgroup
+
+// A workgroup walks spans of consecutive groups, asking for the next while one is computed.  step_t, step_g: the workgroups'
+// stride in whole rows and groups.  y may be out or res: a thread reads its elements before it writes them.
 template <typename T, bool kDrop>
 __global__ __launch_bounds__(256) void dropout_add_kernel(const T* out, const T* res, T* y, int n_tok, int groups, uint32_t inv,
-                                                          DropArgs a) {
-  constexpr int kSpan = 256 * kDropGroups;
-  const uint64_t total = (uint64_t)n_tok * groups, first = ((uint64_t)blockIdx.y * gridDim.x + blockIdx.x) * kSpan;
-  if (first >= total) return;
-  const uint32_t t0 = (uint32_t)(first / (uint32_t)groups), g0 = (uint32_t)(first % (uint32_t)groups);
+                                                          uint32_t step_t, uint32_t step_g, DropArgs a) {
+  const uint64_t total = (uint64_t)n_tok * groups, stride = (uint64_t)gridDim.x * kDropSpan;
+  uint64_t first = (uint64_t)blockIdx.x * kDropSpan;
+  uint32_t t0 = (uint32_t)(first / (uint32_t)groups), g0 = (uint32_t)(first % (uint32_t)groups);
   const uint64_t offset = kDrop ? drop_offset(a) : 0;
-  float v[kDropGroups][8], r[kDropGroups][8];
+  Raw8<T> raw_out[kDropGroups], raw_res[kDropGroups];
+  auto load = [&](uint64_t at) {
 #pragma unroll
-  for (int u = 0; u < kDropGroups; ++u) {
-    const uint64_t i = first + u * 256 + threadIdx.x;
-    if (i >= total) continue;
-    Vec8<T>::load(out + i * 8, v[u]);
-    if (res) Vec8<T>::load(res + i * 8, r[u]);
-  }
-#pragma unroll
-  for (int u = 0; u < kDropGroups; ++u) {
-    const uint64_t i = first + u * 256 + threadIdx.x;
-    if (i >= total) continue;
-    if (kDrop) {
-      const uint32_t w = g0 + u * 256 + threadIdx.x, dt = (uint32_t)tile_div((int)w, groups, inv);
-      drop8(a, offset, t0 + dt, w - dt * groups, v[u]);
+    for (int u = 0; u < kDropGroups; ++u) {
+      const uint64_t i = at + u * 256 + threadIdx.x;
+      if (i >= total) continue;
+      raw_out[u].load(out + i * 8);
+      if (res) raw_res[u].load(res + i * 8);
     }
-    if (res) {
+  };
+#pragma unroll
+  for (int u = 0; u < kDropGroups; ++u) {
+    raw_out[u].clear();
+    raw_res[u].clear();
+  }
+  load(first);
+  for (; first < total; first += stride) {
+    float v[kDropGroups][8], r[kDropGroups][8];
+#pragma unroll
+    for (int u = 0; u < kDropGroups; ++u) {
+      raw_out[u].widen(v[u]);
+      raw_res[u].widen(r[u]);
+    }
+    load(first + stride);
+#pragma unroll
+    for (int u = 0; u < kDropGroups; ++u) {
+      const uint64_t i = first + u * 256 + threadIdx.x;
+      if (kDrop) {
+        const uint32_t w = g0 + u * 256 + threadIdx.x, dt = (uint32_t)tile_div((int)w, groups, inv);
+        drop8(a, offset, t0 + dt, w - dt * groups, v[u]);
+      }
 #pragma unroll
       for (int z = 0; z < 8; ++z) v[u][z] += r[u][z];
+      if (i < total) Vec8<T>::store(y + i * 8, v[u]);
     }
-    Vec8<T>::store(y + i * 8, v[u]);
+    t0 += step_t;
+    g0 += step_g;
+    if (g0 >= (uint32_t)groups) {
+      g0 -= groups;
+      ++t0;
+    }
   }
 }
 

@@ -13,32 +13,6 @@
 
 namespace meft {
 
-template <typename T>
-struct Raw8 {
-  u32x4 w[sizeof(T) / 2];
-  __device__ __forceinline__ void load(const T* p) {
-#pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) w[i] = reinterpret_cast<const u32x4*>(p)[i];
-  }
-  __device__ __forceinline__ void clear() {
-#pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) w[i] = u32x4{0u, 0u, 0u, 0u};
-  }
-  // what was widened from the words is not kept beyond here: it is widened from them again
-  __device__ __forceinline__ void forget() {
-#pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) asm volatile("" : "+v"(w[i]));
-  }
-  __device__ __forceinline__ void widen(float (&v)[8]) const {
-    if constexpr (sizeof(T) == 2) {
-      Vec8<bf16_t>::widen(w[0], v);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i / 4][i % 4]);
-    }
-  }
-};
-
 // v as it is stored in T
 template <typename T>
 __device__ __forceinline__ void round8(float (&v)[8]) {
