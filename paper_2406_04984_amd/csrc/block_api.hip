@@ -246,7 +246,8 @@ template <typename T, int M>
 void launch_route_grad(const RouteGradArgs<T>& a, int wgs, int lds, hipStream_t st) {
   static std::once_flag configured;
   std::call_once(configured, [] {
-    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&route_grad_kernel<T, M>), hipFuncAttributeMaxDynamicSharedMemorySize, kDhLds);
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&route_grad_kernel<T, M>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                              kDhLds + kDhDsLds);
   });
   MEFT_LAUNCH("route_grad", (route_grad_kernel<T, M>), dim3((unsigned)wgs), dim3(64 * kRgWaves), lds, st, a);
 }
@@ -262,12 +263,12 @@ meft_status route_bwd(const meft_shape& s, const void* h, const void* Wg, const 
   const int64_t rounds = ((int64_t)s.T + 32 * kRgWaves - 1) / (32 * kRgWaves), most = (kCus + p.slices - 1) / p.slices;
   const int n_along = (int)(rounds < most ? rounds : most), n_dh = dh ? n_along * p.slices : 0;
   if (n_dw + n_dh == 0) return MEFT_OK;
-  const RouteGradArgs<T> a{static_cast<const T*>(h), static_cast<const T*>(Wg), static_cast<const T*>(add), ds, static_cast<T*>(dh),
-                           static_cast<T*>(dWg), dbias, w.part, w.part_bias, s.T, s.d, s.n_blocks, p.m_shift, p.splits,
-                           p.per_split, n_dw, dw_slices, n_along};
-  const int all = dh_steps<T>(s.n_blocks) * dh_step_bytes<T>(), dh_lds = all < kDhLds ? all : kDhLds;
+  const int all = dh_steps<T>(s.n_blocks) * dh_step_bytes<T>(), w_lds = all < kDhLds ? all : kDhLds, dh_lds = w_lds + kDhDsLds;
   const int dw_lds = p.m_shift == 2 ? 4 << 10 : 2 * p.m * 16 << 10;   // two of M * 64 x 64 sums, or the biases
   const int lds = dh && dh_lds > dw_lds ? dh_lds : dw_lds;
+  const RouteGradArgs<T> a{static_cast<const T*>(h), static_cast<const T*>(Wg), static_cast<const T*>(add), ds, static_cast<T*>(dh),
+                           static_cast<T*>(dWg), dbias, w.part, w.part_bias, s.T, s.d, s.n_blocks, p.m_shift, p.splits,
+                           p.per_split, w_lds / 16, n_dw, dw_slices, n_along};
   if (p.m == 1) launch_route_grad<T, 1>(a, n_dw + n_dh, lds, st);
   else launch_route_grad<T, 2>(a, n_dw + n_dh, lds, st);
   if (dw && p.splits > 1) {

@@ -102,6 +102,7 @@ struct RouteGradArgs {
   float *dbias, *part, *part_bias;   // part: [split][B][d], where there is more than one split
   int n_tok, d, B;
   int m_shift, splits, per_split;    // dWg: 2^m_shift waves along the blocks, splits of the tokens, tokens of a split (a multiple of 16)
+  int dh_words;                      // of 16 bytes, the router's part of LDS; ds is behind it
   int n_dw, dw_slices, n_along;      // workgroups of dWg, their slices of columns (1 where only dbias is wanted); dh's along the tokens
 };
 
@@ -132,9 +133,21 @@ struct StepWords<bf16_t> {
 #pragma unroll
     for (int j = 0; j < 4; ++j) lds[j * 64 + lane] = __builtin_bit_cast(u32x4, w.operand(j));
   }
-  static __device__ __forceinline__ void mma(const float (&x)[8], const u32x4* lds, int lane, f32x16 (&acc)[4]) {
-    u32x4 hi, lo;
-    split(x, hi, lo);
+  // four values of ds, blocks 4 q .. 4 q + 3 (q < 4) of a step, into the left operand's words: high parts, then low parts
+  static __device__ __forceinline__ void put_ds(u32x4* step, int row, int q, u32x4 x) {
+    u32x2 hi, lo;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float a = __uint_as_float(x[2 * i]), b = __uint_as_float(x[2 * i + 1]);
+      hi[i] = pack_bf16x2(a, b);
+      lo[i] = pack_bf16x2(a - __uint_as_float(hi[i] << 16), b - __uint_as_float(hi[i] & 0xFFFF0000u));
+    }
+    u32x2* at = reinterpret_cast<u32x2*>(step + (q >> 1) * 32 + row) + (q & 1);
+    at[0] = hi;
+    at[128] = lo;
+  }
+  static __device__ __forceinline__ void mma(const u32x4* step, const u32x4* lds, int lane, f32x16 (&acc)[4]) {
+    const u32x4 hi = step[lane], lo = step[64 + lane];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const bf16x8 b = __builtin_bit_cast(bf16x8, lds[j * 64 + lane]);
@@ -150,12 +163,14 @@ struct StepWords<float> {
 #pragma unroll
     for (int u = 0; u < 8; ++u) lds[u * 64 + lane] = __builtin_bit_cast(u32x4, w.w[u]);
   }
-  static __device__ __forceinline__ void mma(const float (&x)[8], const u32x4* lds, int lane, f32x16 (&acc)[4]) {
+  static __device__ __forceinline__ void put_ds(u32x4* step, int row, int q, u32x4 x) { step[(q & 1) * 64 + (q >> 1) * 32 + row] = x; }
+  static __device__ __forceinline__ void mma(const u32x4* step, const u32x4* lds, int lane, f32x16 (&acc)[4]) {
+    const u32x4 x[2] = {step[lane], step[64 + lane]};
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       const f32x4 b = __builtin_bit_cast(f32x4, lds[u * 64 + lane]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[u], b[j], acc[j], 0, 0, 0);
+      for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x[u / 4][u % 4]), b[j], acc[j], 0, 0, 0);
     }
   }
 };
@@ -167,6 +182,7 @@ constexpr int dh_ahead() { return sizeof(T) == 2 ? 4 : 2; }
 template <typename T>
 constexpr int dh_steps(int n_blocks) { return (n_blocks + 16 * dh_ahead<T>() - 1) / (16 * dh_ahead<T>()) * dh_ahead<T>(); }
 constexpr int kDhLds = 128 << 10;   // most of LDS that a workgroup's part of the router takes
+constexpr int kDhDsLds = kRgWaves * 2 * 128 * 16;   // two steps of ds for each wave
 template <typename T>
 constexpr int dh_step_bytes() { return StepWords<T>::kUnits * 64 * 16; }
 
@@ -187,7 +203,6 @@ __device__ __forceinline__ void route_dh(const RouteGradArgs<T>& a, int along, i
   constexpr int kAhead = dh_ahead<T>();
   const int steps = dh_steps<T>(a.B);
   const uint32_t o = 4 * half * row_bytes + (c < a.d ? c_bytes : kNoColumn);
-  const uint32_t ds_off = (uint32_t)col * a.B * 4u + 32u * half;
 
   auto stage = [&](int first, int n) {   // steps first .. first + n - 1 of the router
     for (int s = wave; s < n; s += kRgWaves) {
@@ -199,16 +214,20 @@ __device__ __forceinline__ void route_dh(const RouteGradArgs<T>& a, int along, i
       Words::put(s_w + s * Words::kUnits * 64, w, lane);
     }
   };
-  // eight values of ds of this lane's token; blocks and tokens that are not there are 0
-  auto load_ds = [&](__amdgpu_buffer_rsrc_t ds, int s, u32x4(&x)[2]) {
-    const int b = 16 * s + 8 * half;
-    if (kQuads) {
+  // Two steps of ds, 32 blocks of 32 tokens: eight lanes a row, so that a load takes whole lines (a row per lane, as the operand
+  // has them, touches as many lines as a load has lanes times a quarter).  Blocks and tokens that are not there are 0.
+  auto load_ds = [&](__amdgpu_buffer_rsrc_t ds, int s, u32x4(&x)[4]) {
+    const int b = 16 * s + 4 * (lane & 7);
+    const uint32_t at = (uint32_t)(lane >> 3) * a.B * 4u + b * 4u;
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-        x[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ds, (int)(b + 4 * i < a.B ? ds_off + 64 * s + 16 * i : kNoColumn), 0, 0));
-    } else {   // a word of four might run over the row's end
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t o8 = at + 8u * i * a.B * 4u;
+      if (kQuads) {
+        x[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ds, (int)(b < a.B ? o8 : kNoColumn), 0, 0));
+      } else {   // a word of four might run over the row's end
 #pragma unroll
-      for (int u = 0; u < 8; ++u) x[u / 4][u % 4] = __builtin_amdgcn_raw_buffer_load_b32(ds, (int)(b + u < a.B ? ds_off + 64 * s + 4 * u : kNoColumn), 0, 0);
+        for (int u = 0; u < 4; ++u) x[i][u] = __builtin_amdgcn_raw_buffer_load_b32(ds, (int)(b + u < a.B ? o8 + 4 * u : kNoColumn), 0, 0);
+      }
     }
   };
   const int64_t tile0 = (int64_t)along * kRgWaves + wave, n_tiles = ((int64_t)a.n_tok + 31) / 32;
@@ -216,7 +235,8 @@ __device__ __forceinline__ void route_dh(const RouteGradArgs<T>& a, int along, i
   auto tile_rows = [&](int64_t tile) { return tile < 0 ? 0 : (int)max((int64_t)0, min((int64_t)32, a.n_tok - tile * 32)); };
   auto ds_of = [&](int64_t tile) { return rows_at(a.ds + (size_t)tile * 32 * a.B, tile_rows(tile), a.B * 4u); };
 
-  u32x4 x[kAhead][2];
+  u32x4 x[kAhead / 2][4];
+  u32x4* const s_ds = s_w + a.dh_words + wave * (2 * 128);   // this wave's
   typename Rows::Quad y[16];   // 0 where nothing is added
   auto load_add = [&](int64_t tile) {
     const __amdgpu_buffer_rsrc_t add = rows_at(a.add + (a.add ? (size_t)tile * 32 * a.d : 0), a.add ? tile_rows(tile) : 0, row_bytes);
@@ -227,12 +247,16 @@ __device__ __forceinline__ void route_dh(const RouteGradArgs<T>& a, int along, i
   // kAhead steps from s0 on, whose router is at `w`; their places in x then take the same steps of another part or tile
   auto group = [&](const u32x4* w, __amdgpu_buffer_rsrc_t next, int next_s0, bool real = true) {
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      float f[8];
+    for (int i = 0; i < kAhead / 2; ++i) {
+      wave_lds_fence();
 #pragma unroll
-      for (int z = 0; z < 8; ++z) f[z] = __uint_as_float(x[i][z / 4][z % 4]);
-      if (real) Words::mma(f, w + i * Words::kUnits * 64, lane, acc);
-      load_ds(next, next_s0 + i, x[i]);
+      for (int k = 0; k < 4; ++k) Words::put_ds(s_ds + (lane >> 2 & 1) * 128, 8 * k + (lane >> 3), lane & 3, x[i][k]);
+      load_ds(next, next_s0 + 2 * i, x[i]);
+      wave_lds_fence();
+      if (real) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) Words::mma(s_ds + k * 128, w + (2 * i + k) * Words::kUnits * 64, lane, acc);
+      }
       __builtin_amdgcn_sched_barrier(0);
     }
   };
@@ -260,7 +284,7 @@ __device__ __forceinline__ void route_dh(const RouteGradArgs<T>& a, int along, i
     const int pieces = (steps + kMaxSteps - 1) / kMaxSteps;
     if (pieces == 1) stage(0, steps);
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) load_ds(ds_of(tile0), i, x[i]);
+    for (int i = 0; i < kAhead / 2; ++i) load_ds(ds_of(tile0), 2 * i, x[i]);
     load_add(tile0);
     if (pieces == 1) __syncthreads();
     // every wave of the workgroup makes as many rounds as the first: there may be barriers in them
@@ -287,7 +311,7 @@ __device__ __forceinline__ void route_dh(const RouteGradArgs<T>& a, int along, i
     stage(0, kAhead);
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) x[i][0] = x[i][1] = u32x4{0u, 0u, 0u, 0u};
+    for (int i = 0; i < kAhead / 2; ++i) x[i][0] = x[i][1] = x[i][2] = x[i][3] = u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
     for (int r = 0; r < 16; ++r) y[r] = typename Rows::Quad{};
     for (int64_t tile = tile0 - stride; tile < n_tiles; tile += stride) {
