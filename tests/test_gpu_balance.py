@@ -12,7 +12,7 @@ from tests.within import U, assert_guard, assert_within, guarded, host64
 pytestmark = pytest.mark.gpu
 
 SIZES = [(1, 1, 1), (1, 64, 4), (3, 5, 2), (64, 64, 4), (777, 64, 4), (130, 100, 3), (2048, 256, 8), (50, 300, 5), (37, 1000, 16),
-         (33, 1024, 2), (41, 1025, 3), (20, 2048, 8), (9, 4097, 2), (300, 5000, 4), (5, 16384, 300), (4000, 7, 7)]
+         (33, 1024, 2), (41, 1025, 3), (20, 2048, 8), (6, 3000, 5), (9, 4097, 2), (300, 5000, 4), (5, 16384, 300), (4000, 7, 7)]
 
 
 def _inputs(T, nb, e, kind):

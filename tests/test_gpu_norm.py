@@ -164,6 +164,27 @@ def test_add_norm(T, d, dtype, kind, p):
     assert torch.equal(b, dres) and torch.equal(a, dout)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_add_norm_without_dropout(dtype):
+    """No dropout given (serving): the same as a share of 0, forward and backward."""
+    import torch
+    from paper_2406_04984_amd import binding as B
+    T, d = 3, 4096
+    r = np.random.RandomState(9)
+    s, hp, none = _shape(B, T, d, dtype), B.MeftNorm(B.MEFT_NORM_RMS, EPS), B.MeftDrop(0.0, 5, 6)
+    (x, _), (o, _), (g, _), (dh, _) = (dev(r.standard_normal(n), dtype) for n in ((T, d), (T, d), (d,), (T, d)))
+    got = []
+    for drop in (None, none):
+        y, h, rs = torch.zeros_like(x), torch.zeros_like(x), torch.zeros(T, device="cuda")
+        dres, dout, dg = torch.zeros_like(x), torch.zeros_like(x), torch.zeros_like(g)
+        ws = torch.empty((B.meft_block_workspace_bytes(s),), dtype=torch.uint8, device="cuda")
+        B.meft_add_norm_fwd(s, hp, drop, None, o, x, g, None, y, h, None, rs)
+        B.meft_add_norm_bwd(s, hp, drop, None, y, g, None, rs, dh, None, dres, dout, dg, None, ws)
+        assert torch.equal(dres, dout) and bool(dres.any())
+        got.append((y, h, rs, dres, dg))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
 def test_a_row_that_is_no_number_stays_alone():
     import torch
     from paper_2406_04984_amd import binding as B

@@ -12,7 +12,7 @@ from tests.within import U, assert_guard, assert_within, dev, guarded, host64
 pytestmark = pytest.mark.gpu
 
 SIZES = [(1, 8, 1), (1, 4096, 64), (3, 72, 5), (16, 128, 32), (17, 136, 33), (64, 64, 64), (65, 120, 65), (1000, 768, 32),
-         (777, 1000, 64), (300, 264, 130), (255, 512, 256), (70, 384, 300), (33, 256, 1030), (2049, 2048, 48), (513, 4096, 100)]
+         (777, 1000, 64), (300, 264, 130), (255, 512, 256), (70, 384, 300), (33, 256, 1030), (2049, 2048, 48), (513, 4096, 100), (40, 264, 640), (5000, 1024, 602)]
 
 
 def _slack(dtype, terms, n):
