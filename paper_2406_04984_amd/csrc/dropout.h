@@ -68,7 +68,7 @@ struct Raw8 {
   }
 };
 
-constexpr int kDropGroups = 2;                    // groups of eight columns per thread and round
+constexpr int kDropGroups = 1;                    // groups of eight columns per thread and round
 constexpr int kDropSpan = 256 * kDropGroups;      // of a workgroup
 
 // A workgroup walks spans of consecutive groups, asking for the next while one is computed.  step_t, step_g: the workgroups'
