@@ -170,18 +170,86 @@ struct NormBwdArgs {
   const float *mean, *rstd;
   T *dx, *dout;
   float* part;   // [workgroup][dgamma, dbeta][d]
+  T *dgamma, *dbeta;
+  int row_wgs;
   int n_tok, d, layer;
   float inv_d;
   DropArgs drop;
 };
 
+// dgamma and dbeta (may be null) of kApartCols columns by one workgroup, over all rows: they need no sums over a
+// row.  What bounds it is the 100 or so lines that a compute unit has on their way, so a line holds as many of its columns as its
+// type allows at 32 (1000 x 768 fp32, 16 / 32 columns: 11.9 / 10.9 us).
+constexpr int kApartCols = 32;
+template <typename T>
+__device__ __forceinline__ void norm_columns(const NormBwdArgs<T>& a, int c0, float* lds /* [waves][kApartCols] */) {
+  constexpr int kRows = 4;   // whose words are on their way together
+  constexpr int kLanes = kApartCols / 8;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, step = blockDim.x / kLanes;
+  const int c = min(c0 + 8 * (lane % kLanes), a.d - 8);
+  float dgamma[8], dbeta[8];
+#pragma unroll
+  for (int z = 0; z < 8; ++z) dgamma[z] = dbeta[z] = 0.f;
+  for (int64_t first = threadIdx.x / kLanes; first < a.n_tok; first += kRows * step) {
+    Raw8<T> y[kRows], dh[kRows];
+    float mean[kRows], rstd[kRows];
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+      const int64_t t = min(first + u * step, (int64_t)a.n_tok - 1);
+      y[u].load(a.y + (size_t)t * a.d + c);
+      dh[u].load(a.dh + (size_t)t * a.d + c);
+      rstd[u] = a.rstd[t];
+      mean[u] = a.layer ? a.mean[t] : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+      float y8[8], g8[8];
+      y[u].widen(y8);
+      dh[u].widen(g8);
+      const bool live = first + u * step < a.n_tok;
+#pragma unroll
+      for (int z = 0; z < 8; ++z) {
+        dgamma[z] += live ? g8[z] * ((y8[z] - mean[u]) * rstd[u]) : 0.f;
+        dbeta[z] += live ? g8[z] : 0.f;
+      }
+    }
+  }
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    float(&acc)[8] = which == 0 ? dgamma : dbeta;
+    T* out = which == 0 ? a.dgamma : a.dbeta;
+    if (!out) continue;
+#pragma unroll
+    for (int z = 0; z < 8; ++z)
+#pragma unroll
+      for (int o = kLanes; o < 64; o *= 2) acc[z] += __shfl_xor(acc[z], o, kWave);
+    __syncthreads();
+    if (lane < kLanes) Vec8<float>::store(lds + wave * kApartCols + lane * 8, acc);
+    __syncthreads();
+    if (threadIdx.x < kApartCols && c0 + (int)threadIdx.x < a.d) {
+      float sum = 0.f;
+      for (int w = 0; w < waves; ++w) sum += lds[w * kApartCols + threadIdx.x];
+      if constexpr (sizeof(T) == 2) out[c0 + threadIdx.x].bits = (uint16_t)pack_bf16x2(sum, 0.f);
+      else out[c0 + threadIdx.x] = sum;
+    }
+  }
+}
+
 // kGrads: 0 dx only, 1 and dgamma, 2 and dbeta.  A workgroup walks rows with the weight's gradient of its columns in
 // registers; the slots of a workgroup are added through LDS, the workgroups by norm_grad_kernel, both in a fixed order.
+// 3 (few rows): dx by the first row_wgs workgroups and the weights' gradients by workgroups of their own, which read the rows
+// again, in one launch instead of two.
 template <typename T, int V, int W, int kMode, int kGrads>
 __global__ __launch_bounds__(64 * W * norm_max_slots(W)) void norm_bwd_kernel(NormBwdArgs<T> a) {
   constexpr int kMaxSlots = norm_max_slots(W);
   __shared__ float s_sum[2 * kMaxSlots * W * 2];
-  __shared__ __attribute__((aligned(16))) float s_acc[kGrads && kMaxSlots > 1 ? 64 * W * V * 8 : 4];
+  constexpr bool kAcc = kGrads == 1 || kGrads == 2;
+  __shared__ __attribute__((aligned(16))) float s_acc[kGrads == 3 ? 16 * kApartCols : kAcc && kMaxSlots > 1 ? 64 * W * V * 8 : 4];
+  const int row_wgs = kGrads == 3 ? a.row_wgs : (int)gridDim.x;
+  if (kGrads == 3 && (int)blockIdx.x >= row_wgs) {
+    norm_columns(a, ((int)blockIdx.x - row_wgs) * kApartCols, s_acc);
+    return;
+  }
   const int slots = blockDim.x / (64 * W), slot = threadIdx.x / (64 * W), q = threadIdx.x % (64 * W), wave = q / 64;
   RowSum<W, kMaxSlots, 2> row_sum{s_sum};
   const uint64_t offset = kMode == kNormDrop ? drop_offset(a.drop) : 0;
@@ -214,7 +282,7 @@ __global__ __launch_bounds__(64 * W * norm_max_slots(W)) void norm_bwd_kernel(No
       if (a.dy) raw_dy[i].load(a.dy + row + c);
     }
   };
-  const int64_t stride = (int64_t)gridDim.x * slots;
+  const int64_t stride = (int64_t)row_wgs * slots;
   constexpr bool kAhead = W < 16;   // 1024 threads have 128 registers each: none for a row to come
   if (kAhead) load((int64_t)blockIdx.x * slots + slot);
   for (int64_t first = (int64_t)blockIdx.x * slots; first < a.n_tok; first += stride) {
@@ -241,8 +309,8 @@ __global__ __launch_bounds__(64 * W * norm_max_slots(W)) void norm_bwd_kernel(No
     auto sums = [&](int i, float(&x8)[8], float(&g8)[8]) {
 #pragma unroll
       for (int z = 0; z < 8; ++z) {
-        if (kGrads > 0) dgamma[i][z] += live ? g8[z] * x8[z] : 0.f;
-        if (kGrads > 1) dbeta[i][z] += live ? g8[z] : 0.f;
+        if (kAcc) dgamma[i][z] += live ? g8[z] * x8[z] : 0.f;
+        if (kGrads == 2) dbeta[i][z] += live ? g8[z] : 0.f;
       }
       weigh(i, g8);
 #pragma unroll
@@ -293,7 +361,7 @@ __global__ __launch_bounds__(64 * W * norm_max_slots(W)) void norm_bwd_kernel(No
       }
     }
   }
-  if constexpr (kGrads > 0) {
+  if constexpr (kAcc) {
     float* p = a.part + (size_t)blockIdx.x * 2 * a.d;
 #pragma unroll
     for (int which = 0; which < kGrads; ++which) {

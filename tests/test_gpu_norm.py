@@ -103,6 +103,12 @@ def test_norm(T, d, dtype, kind):
     want = dht.clone()
     B.meft_norm_bwd(s, hp, xt, gt, mt if layer else None, rt, want, None, want, None, None, ws)
     assert_within("dx", want, R.norm_bwd(x, gamma, mean, rstd, dh, None, layer)[0], _bwd_slack(xh, g, rstd, np.zeros_like(g)))
+    over = dht.clone()
+    dg3, db3 = torch.zeros_like(dgt), torch.zeros_like(dbt)
+    B.meft_norm_bwd(s, hp, xt, gt, mt, rt, over, dyt, over, dg3, db3, ws)
+    assert torch.equal(over, dx)
+    assert_within("dgamma", dg3[0], dgamma, (T + 32) * U * np.abs(dh * xh).sum(0))
+    assert_within("dbeta", db3[0], dbeta, (T + 32) * U * np.abs(dh).sum(0))
     dg2, inplace = torch.zeros_like(dgt), dyt.clone()
     B.meft_norm_bwd(s, hp, xt, gt, mt, rt, dht, inplace, inplace, dg2, None, ws)
     assert torch.equal(dg2, dgt) and torch.equal(inplace, dx)
@@ -162,6 +168,12 @@ def test_add_norm(T, d, dtype, kind, p):
     a, b = dht.clone(), dyt.clone()
     B.meft_add_norm_bwd(s, hp, drop, step, y, gt, mt, rt, a, b, b, a, None, None, ws)
     assert torch.equal(b, dres) and torch.equal(a, dout)
+    for one, two in ((0, 1), (1, 0)):       # dres or dout in place of dh, with the weights' gradients
+        bufs = [dht.clone(), torch.zeros_like(dht)]
+        B.meft_add_norm_bwd(s, hp, drop, step, y, gt, mt, rt, bufs[0], dyt, bufs[one], bufs[two], dg, db, ws)
+        assert torch.equal(bufs[one], dres) and torch.equal(bufs[two], dout)
+        assert_within("dgamma", dg, dgamma, (T + 32) * U * np.abs(dh * xh).sum(0))
+        assert_within("dbeta", db, dbeta, (T + 32) * U * np.abs(dh).sum(0))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
