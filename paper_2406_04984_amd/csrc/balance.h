@@ -127,17 +127,34 @@ struct BalancePart {
   uint32_t* ticket;
 };
 
+struct BalanceOut {
+  int32_t *counts, *n_valid;
+  float *prob, *loss;
+  float balance, z;
+};
+
+// n tokens, sum of the squared log sums, sum over the blocks of counts times probabilities
+__device__ __forceinline__ void balance_finish(const BalanceOut& out, int n, float lse2, float dot, int B, int e) {
+  const float inv = n > 0 ? 1.f / (float)n : 0.f;
+  const float lb = (float)B / (float)e * dot * inv * inv, lz = lse2 * inv;
+  *out.n_valid = n;
+  // a term of weight 0 is left out, so that an overflow of the other's does not reach the sum
+  out.loss[0] = (out.balance != 0.f ? out.balance * lb : 0.f) + (out.z != 0.f ? out.z * lz : 0.f);
+  out.loss[1] = lb;
+  out.loss[2] = lz;
+}
+
 // Waves of a workgroup where a wave has a row to itself (W == 1): their probabilities meet in LDS.
 constexpr int balance_rows(int w, int z) { return w > 1 ? 1 : z <= 4 ? 16 : 8; }
 template <int Z, int W>
 constexpr int balance_threads() { return 64 * W * balance_rows(W, Z); }
 
-// A row is asked for while the one before is computed.  LDS: counts [B] ints, then for W == 1 the waves' probabilities [waves][B].
+// A row is asked for while the one before is computed.  A workgroup that is alone (W == 1 only) finishes the loss itself.  LDS: counts [B] ints, then for W == 1 the waves' probabilities [waves][B].
 template <int Z, int W>
 __global__ __launch_bounds__((balance_threads<Z, W>())) void balance_part_kernel(const float* __restrict__ scores,
                                                                                  const int32_t* __restrict__ block_idx,
                                                                                  const uint8_t* __restrict__ valid, int n_tok, int B,
-                                                                                 int e, BalancePart part) {
+                                                                                 int e, BalancePart part, BalanceOut out) {
   typedef RowMap<Z, W> Map;
   extern __shared__ int32_t s_cnt[];
   constexpr int kThreads = balance_threads<Z, W>(), kRows = balance_rows(W, Z);
@@ -145,7 +162,8 @@ __global__ __launch_bounds__((balance_threads<Z, W>())) void balance_part_kernel
   __shared__ int32_t s_tok[16];
   const int tid = threadIdx.x, lane0 = W == 1 ? (tid & 63) : tid, slot = W == 1 ? tid / 64 : 0;
   for (int b = tid; b < B; b += kThreads) s_cnt[b] = 0;
-  if (blockIdx.x == 0 && tid == 0) *part.ticket = 0u;   // of the next launch
+  const bool alone = W == 1 && gridDim.x == 1;
+  if (blockIdx.x == 0 && tid == 0 && !alone) *part.ticket = 0u;   // of the next launch
   __syncthreads();
   float acc[Z], next[Z], lse2 = 0.f;
   int n = 0, valid_next = 0, idx_next = -1;
@@ -184,20 +202,33 @@ __global__ __launch_bounds__((balance_threads<Z, W>())) void balance_part_kernel
     if (lane0 == 0) { s_lse2[slot] = lse2; s_tok[slot] = n; }
   }
   __syncthreads();
-  float* prob = part.prob + (size_t)blockIdx.x * B;
-  int32_t* count = part.count + (size_t)blockIdx.x * B;
+  float* prob = alone ? out.prob : part.prob + (size_t)blockIdx.x * B;
+  int32_t* count = alone ? out.counts : part.count + (size_t)blockIdx.x * B;
   if constexpr (W == 1) {
+    float dot = 0.f;
     for (int b = tid; b < B; b += kThreads) {
       float p = 0.f;
 #pragma unroll
       for (int w = 0; w < kRows; ++w) p += s_prob[w * B + b];
       prob[b] = p;
+      dot += p * (float)s_cnt[b];
+    }
+    if (alone) {
+      dot = wave_total(dot);
+      if (lane0 == 0) s_join[slot] = dot;
+      __syncthreads();
     }
     if (tid == 0) {
       lse2 = 0.f;
       n = 0;
 #pragma unroll
       for (int w = 0; w < kRows; ++w) { lse2 += s_lse2[w]; n += s_tok[w]; }
+      if (alone) {
+        dot = 0.f;
+#pragma unroll
+        for (int w = 0; w < kRows; ++w) dot += s_join[w];
+        balance_finish(out, n, lse2, dot, B, e);
+      }
     }
   } else {
 #pragma unroll
@@ -205,14 +236,12 @@ __global__ __launch_bounds__((balance_threads<Z, W>())) void balance_part_kernel
       if (Map::block(z, lane0) < B) prob[Map::block(z, lane0)] = acc[z];
   }
   for (int b = tid; b < B; b += kThreads) count[b] = s_cnt[b];
-  if (tid == 0) { part.lse2[blockIdx.x] = lse2; part.tokens[blockIdx.x] = n; }
+  if (tid == 0 && !alone) { part.lse2[blockIdx.x] = lse2; part.tokens[blockIdx.x] = n; }
 }
 
 // Joins the workgroups' partial sums, 64 blocks and 16 groups of workgroups per workgroup of 1024 threads; the workgroup
 // that is done last adds the others' shares of the loss up in order.
-__global__ __launch_bounds__(1024) void balance_join_kernel(BalancePart part, int n_part, int B, int e, float balance, float z,
-                                                            int32_t* __restrict__ counts, int32_t* __restrict__ n_valid,
-                                                            float* __restrict__ prob, float* __restrict__ loss) {
+__global__ __launch_bounds__(1024) void balance_join_kernel(BalancePart part, int n_part, int B, int e, BalanceOut out) {
   __shared__ float s_prob[16][64], s_lse2[16];
   __shared__ int32_t s_cnt[16][64], s_tok[16];
   __shared__ uint32_t s_last;
@@ -240,7 +269,7 @@ __global__ __launch_bounds__(1024) void balance_join_kernel(BalancePart part, in
   c = 0;
 #pragma unroll
   for (int i = 0; i < 16; ++i) { p += s_prob[i][lane]; c += s_cnt[i][lane]; }
-  if (b < B) { prob[b] = p; counts[b] = c; }
+  if (b < B) { out.prob[b] = p; out.counts[b] = c; }
   float dot = wave_sum(p * (float)c);
   if (gridDim.x > 1) {
     uint32_t last = 0u;
@@ -258,13 +287,7 @@ __global__ __launch_bounds__(1024) void balance_join_kernel(BalancePart part, in
     n = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) { l2 += s_lse2[i]; n += s_tok[i]; }
-    const float inv = n > 0 ? 1.f / (float)n : 0.f;
-    const float lb = (float)B / (float)e * dot * inv * inv, lz = l2 * inv;
-    *n_valid = n;
-    // a term of weight 0 is left out, so that an overflow of the other's does not reach the sum
-    loss[0] = (balance != 0.f ? balance * lb : 0.f) + (z != 0.f ? z * lz : 0.f);
-    loss[1] = lb;
-    loss[2] = lz;
+    balance_finish(out, n, l2, dot, B, e);
   }
 }
 

@@ -173,8 +173,11 @@ constexpr int kDropWgs = 8 * kCus;   // workgroups of dropout_add at most
 // ---- balance --------------------------------------------------------------------------------
 // waves of a row of scores, and the scores of a lane
 int balance_waves(const meft_shape& s) { return s.n_blocks <= 1024 ? 1 : 16; }
+// Few rows for each wave of one workgroup: it is alone and finishes the loss, one launch less (forward + backward, us, alone / with
+// the join: 128 tokens, 64 blocks 13.0 / 16.9, 256 blocks 13.3 / 16.1; 16 tokens, 1000 blocks 12.6 / 15.6, 64 tokens 18.1 / 16.8).
 int balance_grid(const meft_shape& s) {
   const int rows = balance_rows(balance_waves(s), s.n_blocks <= 256 ? 4 : 16);
+  if (balance_waves(s) == 1 && s.T <= (s.n_blocks <= 256 ? 8 : 2) * rows) return 1;
   const int64_t need = ((int64_t)s.T + rows - 1) / rows;
   return (int)(need < 1 ? 1 : need < kCus ? need : kCus);
 }
@@ -208,7 +211,7 @@ static_assert(kMaxBlocks <= 16 * 16 * 64, "balance_part_kernel and balance_grad_
 
 template <int Z, int W>
 void launch_balance_part(const meft_shape& s, const float* scores, const int32_t* block_idx, const uint8_t* valid,
-                         const BalancePart& part, hipStream_t st) {
+                         const BalancePart& part, const BalanceOut& out, hipStream_t st) {
   constexpr int rows = balance_rows(W, Z);
   const size_t lds = (size_t)s.n_blocks * 4 * (W == 1 ? rows + 1 : 1);
   if (W > 1) {
@@ -219,13 +222,13 @@ void launch_balance_part(const meft_shape& s, const float* scores, const int32_t
     });
   }
   MEFT_LAUNCH("balance_part", (balance_part_kernel<Z, W>), dim3(balance_grid(s)), dim3(balance_threads<Z, W>()), lds, st, scores,
-              block_idx, valid, s.T, s.n_blocks, s.top_e, part);
+              block_idx, valid, s.T, s.n_blocks, s.top_e, part, out);
 }
 
 bool balance_ok(const meft_balance* b) { return b && std::isfinite(b->balance) && std::isfinite(b->z); }
 
 // ---- router gradient ------------------------------------------------------------------------
-constexpr int kDwWgs = kCus;   // workgroups of dWg to aim at
+constexpr int kDwWgs = kCus;   // workgroups of dWg at most, where one of all tokens does not need more
 struct RouteGradPlan {
   int slices, m, m_shift, groups, splits, per_split;
 };
@@ -237,12 +240,19 @@ RouteGradPlan route_grad_plan(const meft_shape& s) {
   while ((1 << p.m_shift) < tiles && (1 << p.m_shift) < kRgWaves) ++p.m_shift;
   const int m_waves = 1 << p.m_shift;
   p.groups = (tiles + m_waves - 1) / m_waves;
-  // as many splits of the tokens as give every compute unit a workgroup, each at least 16 tokens per wave
-  const int64_t least = 16 * (kRgWaves / m_waves), want = (kDwWgs + p.slices * p.groups - 1) / (p.slices * p.groups);
-  const int64_t can = (s.T + least - 1) / least;
-  int64_t splits = want < can ? want : can;
-  if (splits < 1) splits = 1;
-  const int64_t per = ((s.T + splits - 1) / splits + 15) / 16 * 16;
+  // Splits of the tokens: what a wave's steps take, each split's partial sums on their way out and in, and the launch that adds
+  // them, in us; at most a workgroup for every compute unit.  Whole call, us, splits of at least one step / by this: 256 tokens,
+  // d 2048, 256 blocks 22.2 (16 splits) / 11.7 (1), 256 tokens, d 4096, 64 blocks 11.8 (4) / 8.0 (1), 2048 tokens, d 2048, 512 blocks 40.7 / 37.8.
+  const double step_us = s.dtype == MEFT_BF16 ? 0.5 : 1.2 * p.m, part_us = 8.0 * s.n_blocks * (double)s.d / 5e6;
+  const int64_t want = (kDwWgs + p.slices * p.groups - 1) / (p.slices * p.groups), steps = ((int64_t)s.T + 15) / 16;
+  const int k_waves = kRgWaves / m_waves;
+  int64_t splits = 1;
+  double best = 0;
+  for (int64_t n = 1; n <= want && (n == 1 || n * k_waves <= steps); ++n) {
+    const double us = (double)((steps + n * k_waves - 1) / (n * k_waves)) * step_us + (n > 1 ? n * part_us + 3.5 : 0);
+    if (n == 1 || us < best) { best = us; splits = n; }
+  }
+  const int64_t per = (((int64_t)s.T + splits - 1) / splits + 15) / 16 * 16;
   p.per_split = (int)(per < 16 ? 16 : per);
   splits = ((int64_t)s.T + p.per_split - 1) / p.per_split;
   p.splits = (int)(splits < 1 ? 1 : splits);
@@ -435,13 +445,15 @@ meft_status meft_balance_fwd(const meft_shape* shape, const meft_balance* balanc
   if ((rc = check_block_ws(s, ws, ws_bytes)) != MEFT_OK) return rc;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const BalanceWs w(s, ws);
+  const BalanceOut out{counts, n_valid, prob, loss, balance->balance, balance->z};
   MEFT_API_LOCK();
   clear_stale_error();
-#define X(Z, W) launch_balance_part<Z, W>(s, scores, block_idx, valid, w, st)
+#define X(Z, W) launch_balance_part<Z, W>(s, scores, block_idx, valid, w, out, st)
   MEFT_BALANCE_SHAPES(X);
 #undef X
-  MEFT_LAUNCH("balance_join", balance_join_kernel, dim3((s.n_blocks + 63) / 64), dim3(1024), 0, st, static_cast<const BalancePart&>(w),
-              balance_grid(s), s.n_blocks, s.top_e, balance->balance, balance->z, counts, n_valid, prob, loss);
+  if (balance_waves(s) > 1 || balance_grid(s) > 1)
+    MEFT_LAUNCH("balance_join", balance_join_kernel, dim3((s.n_blocks + 63) / 64), dim3(1024), 0, st, static_cast<const BalancePart&>(w),
+                balance_grid(s), s.n_blocks, s.top_e, out);
   return launch_status();
 }
 
