@@ -433,7 +433,7 @@ typedef struct {
  * probability is 0.  A token whose scores are all -inf is not valid.  With no valid token everything is 0.
  *   scores    [T, n_blocks] f32  in
  *   block_idx [T, top_e] i32     in   as meft_route writes it; ids outside [0, n_blocks) are not counted
- *   valid     [T] u8             in   0 for tokens that only pad the batch, whose rows are then not read; NULL: all are valid
+ *   valid     [T] u8             in   0 for tokens that only pad the batch, whatever their rows hold; NULL: all are valid
  *   counts    [n_blocks] i32     out
  *   n_valid   [1] i32            out
  *   prob      [n_blocks] f32     out  sum over the valid tokens of P[t, b]

@@ -190,10 +190,9 @@ template <typename T>
 constexpr int dh_step_bytes() { return StepWords<T>::kUnits * 64 * 16; }
 
 // dh.  A workgroup holds the router's rows of 128 columns in LDS, as operands, and walks tiles of 32 tokens per wave.  What is
-// added to a tile and its ds are asked for while the tile before is computed.  More blocks than kDhLds holds are staged piece
-// by piece for every tile.  `along` of `n_along` workgroups along the tokens.  kQuads: the number of
-// blocks is a multiple of 4.  kPieces: they are more
-// than one group of steps.
+// added to a tile and its ds are asked for while the tile before is computed.  More blocks than kDhLds holds are staged piece by
+// piece for every tile.  `along` of `n_along` workgroups along the tokens.  kQuads: the number of blocks is a multiple of 4.
+// kPieces: they are more than one group of steps.
 template <typename T, bool kQuads, bool kPieces>
 __device__ __forceinline__ void route_dh(const RouteGradArgs<T>& a, int along, int n_along, int slice, u32x4* s_w) {
   typedef Rows8<T> Rows;
