@@ -11,7 +11,7 @@ from tests.within import U, assert_guard, assert_within, guarded, host64
 
 pytestmark = pytest.mark.gpu
 
-SIZES = [(1, 1, 1), (1, 64, 4), (3, 5, 2), (64, 64, 4), (777, 64, 4), (130, 100, 3), (2048, 256, 8), (50, 300, 5), (37, 1000, 16),
+SIZES = [(1, 1, 1), (1, 64, 4), (3, 5, 2), (64, 64, 4), (777, 64, 4), (130, 100, 3), (2048, 256, 8), (50, 300, 5), (37, 1000, 16), (20, 1000, 100),
          (33, 1024, 2), (41, 1025, 3), (20, 2048, 8), (6, 3000, 5), (9, 4097, 2), (300, 5000, 4), (5, 16384, 300), (4000, 7, 7)]
 
 
@@ -21,7 +21,7 @@ def _inputs(T, nb, e, kind):
     idx = np.argsort(-s, axis=1, kind="stable")[:, :e].astype(np.int32)
     valid = None
     if kind != "all":
-        valid = (r.uniform(size=T) < 0.6).astype(np.uint8)
+        valid = np.where(r.uniform(size=T) < 0.6, r.choice([1, 2, 255], T), 0).astype(np.uint8)
         s[valid == 0] = np.nan                                  # what pads the batch is not looked at
         idx[valid == 0] = 10 ** 9
     if kind == "shut" and nb > 1:

@@ -129,3 +129,33 @@ def test_two_streams_at_once():
     for blk, w in zip((a, b), want):
         got = _outputs(blk)
         assert all(torch.equal(got[n], w[n]) for n in got)
+
+
+def test_two_graphs_at_once():
+    """Two captured steps with workspaces of their own, replayed on two streams at the same time, again and again."""
+    import torch
+    a, b = _block(CASES[1], p=0.0), _block(CASES[0], p=0.0)
+    want, graphs = [], []
+    for blk in (a, b):
+        blk.step()
+        torch.cuda.synchronize()
+        want.append(_outputs(blk))
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            blk.step()
+        graphs.append(g)
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for _ in range(4):
+        for blk in (a, b):
+            for n in OUTPUTS:
+                if getattr(blk, n) is not None:
+                    getattr(blk, n).zero_()
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for g, st in zip(graphs, streams):
+                with torch.cuda.stream(st):
+                    g.replay()
+        torch.cuda.synchronize()
+        for blk, w in zip((a, b), want):
+            got = _outputs(blk)
+            assert all(torch.equal(got[n], w[n]) for n in got)
