@@ -91,6 +91,12 @@ void launch_norm_bwd(const meft_shape& s, const NormBwdArgs<T>& a, hipStream_t s
 #undef X
 }
 
+// Large results go past L2.  us, past / kept, one card, the mean of three runs each: dropout with the residual add 8192 x 4096 bf16
+// 62.5 / 65.8; plain norm, forward + backward, bf16: rms 8192 x 4096 74.3 / 76.7, layer 8192 x 4096 75.6 / 79.6, layer 16384 x 1024
+// 39.1 / 42.5, rms 4096 x 8192 77.7 / 81.5.  Kept in L2: fp32 (layer 4096 x 4096 81.1 / 78.9) and the two results of add and norm
+// (8192 x 4096 bf16 115.5 / 115.1).
+bool past_l2(const meft_shape& s) { return s.dtype == MEFT_BF16 && (int64_t)s.T * s.d * 2 >= (int64_t)32 << 20; }
+
 bool norm_ok(const meft_norm* n) {
   return n && (n->kind == MEFT_NORM_LAYER || n->kind == MEFT_NORM_RMS) && n->eps >= 0.f && std::isfinite(n->eps);
 }
@@ -121,7 +127,7 @@ meft_status norm_fwd(const meft_shape& s, const meft_norm& n, int mode, const Dr
                      const void* gamma, const void* beta, void* y, void* h, float* mean, float* rstd, hipStream_t st) {
   const NormFwdArgs<T> a{static_cast<const T*>(x), static_cast<const T*>(out), static_cast<const T*>(gamma), static_cast<const T*>(beta),
                          static_cast<T*>(y), static_cast<T*>(h), mean, rstd, s.T, s.d, n.kind == MEFT_NORM_LAYER,
-                         (float)(1.0 / s.d), n.eps, drop};
+                         (float)(1.0 / s.d), n.eps, past_l2(s), drop};
   if (mode == kNormPlain) launch_norm_fwd<T, kNormPlain>(s, a, st);
   else if (mode == kNormAdd) launch_norm_fwd<T, kNormAdd>(s, a, st);
   else launch_norm_fwd<T, kNormDrop>(s, a, st);
@@ -158,7 +164,7 @@ meft_status norm_bwd(const meft_shape& s, const meft_norm& n, int mode, const Dr
   const NormBwdArgs<T> a{static_cast<const T*>(y), static_cast<const T*>(gamma), static_cast<const T*>(dh), static_cast<const T*>(dy),
                          mean, rstd, static_cast<T*>(dx), static_cast<T*>(dout), w.part, static_cast<T*>(dgamma), static_cast<T*>(dbeta),
                          norm_apart_rows(s), s.T, s.d, n.kind == MEFT_NORM_LAYER,
-                         (float)(1.0 / s.d), drop};
+                         (float)(1.0 / s.d), past_l2(s), drop};
   if (mode == kNormPlain) norm_bwd_grads<T, kNormPlain>(s, a, grads, st);
   else if (mode == kNormAdd) norm_bwd_grads<T, kNormAdd>(s, a, grads, st);
   else norm_bwd_grads<T, kNormDrop>(s, a, grads, st);
@@ -383,7 +389,7 @@ meft_status meft_dropout_add(const meft_shape* shape, const meft_drop* drop, con
   clear_stale_error();
 #define DROPOUT(TY, DROP) MEFT_LAUNCH("dropout_add", (dropout_add_kernel<TY, DROP>), grid, dim3(256), 0, st, static_cast<const TY*>(out), \
                                      static_cast<const TY*>(res), static_cast<TY*>(y), s.T, groups, tile_div_inverse(groups), \
-                                     step_t, step_g, a)
+                                     step_t, step_g, past_l2(s), a)
   if (s.dtype == MEFT_BF16) {
     if (thr) DROPOUT(bf16_t, true);
     else DROPOUT(bf16_t, false);

@@ -68,16 +68,31 @@ struct Raw8 {
   }
 };
 
+// eight elements; bf16 past L2 where asked
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const float (&v)[8], bool past) {
+  if constexpr (sizeof(T) == 2) {
+    if (past) {
+      asm volatile("");   // here and below: else the compiler makes one of the two stores, the ordinary one
+      Vec16<T>::store(p, v);
+      asm volatile("");
+      return;
+    }
+  }
+  Vec8<T>::store(p, v);
+}
+
 constexpr int kDropGroups = 1;                    // groups of eight columns per thread and round
 constexpr int kDropSpan = 256 * kDropGroups;      // of a workgroup
 
 // Memory bounds it: 20 integer multiplications per eight elements hide behind their 32 to 48 bytes.  8192 x 4096 bf16, p 0.05:
-// 42 us with a residual (4.8 TB/s), 24.5 without (5.5 TB/s); four groups a thread in a grid that covers them all took 47 and 31.
+// 37 us with a residual (5.4 TB/s; 42 with the result kept in L2), 25.7 without (5.2 TB/s); four groups a thread in a grid that
+// covers them all took 47 and 31, results kept in L2.
 // A workgroup walks spans of consecutive groups, asking for the next while one is computed.  step_t, step_g: the workgroups'
 // stride in whole rows and groups.  y may be out or res: a thread reads its elements before it writes them.
 template <typename T, bool kDrop>
 __global__ __launch_bounds__(256) void dropout_add_kernel(const T* out, const T* res, T* y, int n_tok, int groups, uint32_t inv,
-                                                          uint32_t step_t, uint32_t step_g, DropArgs a) {
+                                                          uint32_t step_t, uint32_t step_g, bool past, DropArgs a) {
   const uint64_t total = (uint64_t)n_tok * groups, stride = (uint64_t)gridDim.x * kDropSpan;
   uint64_t first = (uint64_t)blockIdx.x * kDropSpan;
   uint32_t t0 = (uint32_t)(first / (uint32_t)groups), g0 = (uint32_t)(first % (uint32_t)groups);
@@ -115,7 +130,7 @@ __global__ __launch_bounds__(256) void dropout_add_kernel(const T* out, const T*
       }
 #pragma unroll
       for (int z = 0; z < 8; ++z) v[u][z] += r[u][z];
-      if (i < total) Vec8<T>::store(y + i * 8, v[u]);
+      if (i < total) store8(y + i * 8, v[u], past);
     }
     t0 += step_t;
     g0 += step_g;

@@ -65,6 +65,7 @@ struct NormFwdArgs {
   float *mean, *rstd;
   int n_tok, d, layer;
   float inv_d, eps;
+  bool past;   // h past L2 (kNormPlain)
   DropArgs drop;
 };
 
@@ -72,7 +73,7 @@ struct NormFwdArgs {
 constexpr int norm_max_slots(int w) { return w >= 4 ? 1 : 4 / w; }
 
 // Memory bounds it.  A row's words are asked for while the row before is computed: they are widened at the top of a round, and
-// their registers then take the next row's.  8192 x 4096 bf16, rms: 23 us (5.8 TB/s; 26 with each row asked for when its turn
+// their registers then take the next row's.  8192 x 4096 bf16, rms: 25 us (5.3 TB/s; at best 23.7, and 26 with each row asked for when its turn
 // comes); with dropout and the residual add 50 us for twice the bytes.
 template <typename T, int V, int W, int kMode>
 __global__ __launch_bounds__(64 * W * norm_max_slots(W)) void norm_fwd_kernel(NormFwdArgs<T> a) {
@@ -160,7 +161,7 @@ __global__ __launch_bounds__(64 * W * norm_max_slots(W)) void norm_fwd_kernel(No
       beta[i].widen(bt);
 #pragma unroll
       for (int z = 0; z < 8; ++z) v[i][z] = (v[i][z] - mean[0]) * rstd * gm[z] + bt[z];
-      Vec8<T>::store(a.h + row + (i * 64 * W + q) * 8, v[i]);
+      store8(a.h + row + (i * 64 * W + q) * 8, v[i], kMode == kNormPlain && a.past);
     }
   }
 }
@@ -175,6 +176,7 @@ struct NormBwdArgs {
   int row_wgs;
   int n_tok, d, layer;
   float inv_d;
+  bool past;   // dx past L2 (kNormPlain)
   DropArgs drop;
 };
 
@@ -238,7 +240,7 @@ __device__ __forceinline__ void norm_columns(const NormBwdArgs<T>& a, int c0, fl
 
 // kGrads: 0 dx only, 1 and dgamma, 2 and dbeta.  A workgroup walks rows with the weight's gradient of its columns in
 // registers; the slots of a workgroup are added through LDS, the workgroups by norm_grad_kernel, both in a fixed order.
-// Memory bounds it: 8192 x 4096 bf16, rms, 44 us for three matrices read and one written (6.1 TB/s), with dropout's output 57.
+// Memory bounds it: 8192 x 4096 bf16, rms, 43 us for three matrices read and one written (6.2 TB/s), with dropout's output 57.
 // 3 (few rows): dx by the first row_wgs workgroups and the weights' gradients by workgroups of their own, which read the rows
 // again, in one launch instead of two.
 template <typename T, int V, int W, int kMode, int kGrads>
@@ -356,7 +358,7 @@ __global__ __launch_bounds__(64 * W * norm_max_slots(W)) void norm_bwd_kernel(No
       }
 #pragma unroll
       for (int z = 0; z < 8; ++z) g[k][z] = rstd * (g[k][z] - m0 - xh[k][z] * m1) + r[k][z];
-      Vec8<T>::store(a.dx + row + c, g[k]);
+      store8(a.dx + row + c, g[k], kMode == kNormPlain && a.past);
       if (kMode != kNormPlain) {
         if (kMode == kNormDrop) drop8(a.drop, offset, (uint32_t)t, c / 8, g[k]);
         Vec8<T>::store(a.dout + row + c, g[k]);
