@@ -8,7 +8,7 @@
 // valid: it has no softmax.
 //
 // W waves hold a row in registers, Z scores per lane; W = 1 up to 1024 blocks.  What bounds it are a row's vector instructions and,
-// for few rows, the launches.  16384 x 256: partial sums 6 us, their join 5, the gradient 9 (33 MB); 2048 x 64: 3.5, 3.1, 2.8.
+// for few rows, the launches.  16384 x 256: partial sums 7 us, their join 5.5, the gradient 10 (33 MB); 2048 x 64: 3.9, 3.2, 3.3.
 #pragma once
 #include "common.h"
 

@@ -73,8 +73,9 @@ struct NormFwdArgs {
 constexpr int norm_max_slots(int w) { return w >= 4 ? 1 : 4 / w; }
 
 // Memory bounds it.  A row's words are asked for while the row before is computed: they are widened at the top of a round, and
-// their registers then take the next row's.  8192 x 4096 bf16, rms: 25 us (5.3 TB/s; at best 23.7, and 26 with each row asked for when its turn
-// comes); with dropout and the residual add 50 us for twice the bytes.
+// their registers then take the next row's.  8192 x 4096 bf16, rms: 25 us on average (5.3 TB/s); before
+// results went past L2, 24 and 28 with each row asked for when its turn comes.  With dropout and the residual add 53 us for twice
+// the bytes.
 template <typename T, int V, int W, int kMode>
 __global__ __launch_bounds__(64 * W * norm_max_slots(W)) void norm_fwd_kernel(NormFwdArgs<T> a) {
   constexpr int kMaxSlots = norm_max_slots(W);
@@ -240,7 +241,7 @@ __device__ __forceinline__ void norm_columns(const NormBwdArgs<T>& a, int c0, fl
 
 // kGrads: 0 dx only, 1 and dgamma, 2 and dbeta.  A workgroup walks rows with the weight's gradient of its columns in
 // registers; the slots of a workgroup are added through LDS, the workgroups by norm_grad_kernel, both in a fixed order.
-// Memory bounds it: 8192 x 4096 bf16, rms, 43 us for three matrices read and one written (6.2 TB/s), with dropout's output 57.
+// Memory bounds it: 8192 x 4096 bf16, rms, 43 us for three matrices read and one written (6.2 TB/s), with dropout's output 59.
 // 3 (few rows): dx by the first row_wgs workgroups and the weights' gradients by workgroups of their own, which read the rows
 // again, in one launch instead of two.
 template <typename T, int V, int W, int kMode, int kGrads>

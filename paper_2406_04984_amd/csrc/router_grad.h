@@ -8,8 +8,8 @@
 // (it wants eight rows of one column per lane); lane l then holds columns 4 (l % 32) + j of its four result tiles j, so that a
 // result row leaves as one 8- or 16-byte word per lane, 32 lanes on consecutive addresses.
 //
-// 8192 x 4096 bf16, 64 blocks: 45.5 us for 217 MB (4.8 TB/s; a copy in tiles of this shape reaches 5.0 to 5.3) and 4.5 for the join;
-// 4096 x 4096, 256 blocks: 49 and 7 us, there bound by the instructions of dWg's waves and by their loads through the vector cache.
+// 8192 x 4096 bf16, 64 blocks: 47 us for 217 MB (4.6 TB/s; a copy in tiles of this shape reaches 5.0 to 5.3) and 4.9 for the join;
+// 4096 x 4096, 256 blocks: 53 and 8 us, there bound by the instructions of dWg's waves and by their loads through the vector cache.
 //
 // ds arrives in fp32.  bf16 shapes split it in two bf16 parts, high and low, and multiply both: rounded to one, its error would
 // be as large as that of rounding the result; the matrix cores have the time.  fp32 shapes use fp32 matrix instructions.
