@@ -235,6 +235,17 @@ bool balance_ok(const meft_balance* b) { return b && std::isfinite(b->balance) &
 
 // ---- router gradient ------------------------------------------------------------------------
 constexpr int kDwWgs = kCus;   // workgroups of dWg at most, where one of all tokens does not need more
+// LDS of a workgroup of dh: its part of the router, in bytes
+int dh_router_lds(const meft_shape& s) {
+  const int all = s.dtype == MEFT_BF16 ? dh_steps<bf16_t>(s.n_blocks) * dh_step_bytes<bf16_t>()
+                                       : dh_steps<float>(s.n_blocks) * dh_step_bytes<float>();
+  return all < kDhLds ? all : kDhLds;
+}
+// workgroups of dh along the tokens: one for every compute unit beside dWg's, each with at least a tile per wave
+int dh_along(const meft_shape& s, int slices) {
+  const int64_t rounds = ((int64_t)s.T + 32 * kRgWaves - 1) / (32 * kRgWaves), most = (kCus + slices - 1) / slices;
+  return (int)(rounds < most ? rounds : most);
+}
 struct RouteGradPlan {
   int slices, m, m_shift, groups, splits, per_split;
 };
@@ -250,7 +261,16 @@ RouteGradPlan route_grad_plan(const meft_shape& s) {
   // them, in us; at most a workgroup for every compute unit.  Whole call, us, splits of at least one step / by this: 256 tokens,
   // d 2048, 256 blocks 22.2 (16 splits) / 11.7 (1), 256 tokens, d 4096, 64 blocks 11.8 (4) / 8.0 (1), 2048 tokens, d 2048, 512 blocks 40.7 / 37.8.
   const double step_us = s.dtype == MEFT_BF16 ? 0.5 : 1.2 * p.m, part_us = 8.0 * s.n_blocks * (double)s.d / 5e6;
-  const int64_t want = (kDwWgs + p.slices * p.groups - 1) / (p.slices * p.groups), steps = ((int64_t)s.T + 15) / 16;
+  int64_t want = (kDwWgs + p.slices * p.groups - 1) / (p.slices * p.groups);
+  const int64_t steps = ((int64_t)s.T + 15) / 16;
+  // Where a compute unit's 160 KB hold one workgroup only and dh takes up to half of them, dWg's are to run beside dh's and not
+  // before: us, any number of splits / as many as that leaves, fp32, 747 tokens, d 1160, 294 blocks 44.5 / 35.0, 2000 tokens, d 1024,
+  // 256 blocks 46.7 / 32.3.  dh's workgroups in front instead: 35.9 and 38.7, and 42.0 for 40.5 at 512 blocks in bf16.
+  const int n_dh = dh_along(s, p.slices) * p.slices;
+  if (2 * (dh_router_lds(s) + kDhDsLds) > 160 << 10 && n_dh <= kCus / 2) {
+    const int64_t beside = (kCus - n_dh) / (p.slices * p.groups);
+    want = beside < 1 ? 1 : beside;
+  }
   const int k_waves = kRgWaves / m_waves;
   int64_t splits = 1;
   double best = 0;
@@ -294,11 +314,9 @@ meft_status route_bwd(const meft_shape& s, const void* h, const void* Wg, const 
   const RouteGradWs w(s, ws);
   const bool dw = dWg || dbias;
   const int dw_slices = dWg ? p.slices : 1, n_dw = dw ? dw_slices * p.groups * p.splits : 0;
-  // dh: a workgroup for every compute unit beside dWg's, each with at least a tile per wave
-  const int64_t rounds = ((int64_t)s.T + 32 * kRgWaves - 1) / (32 * kRgWaves), most = (kCus + p.slices - 1) / p.slices;
-  const int n_along = (int)(rounds < most ? rounds : most), n_dh = dh ? n_along * p.slices : 0;
+  const int n_along = dh_along(s, p.slices), n_dh = dh ? n_along * p.slices : 0;
   if (n_dw + n_dh == 0) return MEFT_OK;
-  const int all = dh_steps<T>(s.n_blocks) * dh_step_bytes<T>(), w_lds = all < kDhLds ? all : kDhLds, dh_lds = w_lds + kDhDsLds;
+  const int w_lds = dh_router_lds(s), dh_lds = w_lds + kDhDsLds;
   const int dw_lds = p.m_shift == 2 ? 4 << 10 : 2 * p.m * 16 << 10;   // two of M * 64 x 64 sums, or the biases
   const int lds = dh && dh_lds > dw_lds ? dh_lds : dw_lds;
   const RouteGradArgs<T> a{static_cast<const T*>(h), static_cast<const T*>(Wg), static_cast<const T*>(add), ds, static_cast<T*>(dh),
