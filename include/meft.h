@@ -463,7 +463,7 @@ meft_status meft_balance_bwd(const meft_shape* shape, const meft_balance* balanc
  *   dh       [T, d]        out  may be add; may be NULL
  *   dWg      [n_blocks, d] out  may be NULL
  *   dbias    [n_blocks] f32 out may be NULL
- * bf16 shapes split dscores into two bf16 parts and multiply both, so that rounding it does not show next to the result's.
+ * bf16 shapes multiply three bf16 parts of dscores, which together hold its 24 bits: dscores is not rounded.
  */
 meft_status meft_route_bwd(const meft_shape* shape, const void* h, const void* Wg, const float* dscores, const void* add, void* dh,
                            void* dWg, float* dbias, void* ws, size_t ws_bytes, void* stream);

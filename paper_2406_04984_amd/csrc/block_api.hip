@@ -259,13 +259,13 @@ RouteGradPlan route_grad_plan(const meft_shape& s) {
   p.groups = (tiles + m_waves - 1) / m_waves;
   // Splits of the tokens: what a wave's steps take, each split's partial sums on their way out and in, and the launch that adds
   // them, in us; at most a workgroup for every compute unit.  Whole call, us, splits of at least one step / by this: 256 tokens,
-  // d 2048, 256 blocks 22.2 (16 splits) / 11.7 (1), 256 tokens, d 4096, 64 blocks 11.8 (4) / 8.0 (1), 2048 tokens, d 2048, 512 blocks 40.7 / 37.8.
+  // d 2048, 256 blocks 25.2 (16 splits) / 12.9 (1), 256 tokens, d 4096, 64 blocks 12.7 (4) / 8.3 (1); 2048 tokens, d 2048, 512 blocks 49.0 / 49.6.
   const double step_us = s.dtype == MEFT_BF16 ? 0.5 : 1.2 * p.m, part_us = 8.0 * s.n_blocks * (double)s.d / 5e6;
   int64_t want = (kDwWgs + p.slices * p.groups - 1) / (p.slices * p.groups);
   const int64_t steps = ((int64_t)s.T + 15) / 16;
   // Where a compute unit's 160 KB hold one workgroup only and dh takes up to half of them, dWg's are to run beside dh's and not
   // before: us, any number of splits / as many as that leaves, fp32, 747 tokens, d 1160, 294 blocks 44.5 / 35.0, 2000 tokens, d 1024,
-  // 256 blocks 46.7 / 32.3.  dh's workgroups in front instead: 35.9 and 38.7, and 42.0 for 40.5 at 512 blocks in bf16.
+  // 256 blocks 46.7 / 32.3; dh's workgroups in front instead 35.9 and 38.7.
   const int n_dh = dh_along(s, p.slices) * p.slices;
   if (2 * (dh_router_lds(s) + kDhDsLds) > 160 << 10 && n_dh <= kCus / 2) {
     const int64_t beside = (kCus - n_dh) / (p.slices * p.groups);

@@ -8,11 +8,12 @@
 // (it wants eight rows of one column per lane); lane l then holds columns 4 (l % 32) + j of its four result tiles j, so that a
 // result row leaves as one 8- or 16-byte word per lane, 32 lanes on consecutive addresses.
 //
-// 8192 x 4096 bf16, 64 blocks: 47 us for 217 MB (4.6 TB/s; a copy in tiles of this shape reaches 5.0 to 5.3) and 4.9 for the join;
-// 4096 x 4096, 256 blocks: 53 and 8 us, there bound by the instructions of dWg's waves and by their loads through the vector cache.
+// 8192 x 4096 bf16, 64 blocks: 48.5 us for 217 MB (4.5 TB/s; a copy in tiles of this shape reaches 5.0 to 5.3) and 5.1 for the join;
+// 4096 x 4096, 256 blocks: 67 and 8 us, there bound by the instructions of dWg's waves and by their loads through the vector cache.
 //
-// ds arrives in fp32.  bf16 shapes split it in two bf16 parts, high and low, and multiply both: rounded to one, its error would
-// be as large as that of rounding the result; the matrix cores have the time.  fp32 shapes use fp32 matrix instructions.
+// ds arrives in fp32.  bf16 shapes cut it in three bf16 parts of eight bits each, which together are ds (below 2^-110 up to the last bits
+// that bf16's range has), and multiply all three: the products are those of fp32.  Two parts take 50.5 and 55 us there and keep 16 bits.
+// fp32 shapes use fp32 matrix instructions.
 #pragma once
 #include "common.h"
 
@@ -63,26 +64,32 @@ struct Rows8<float> {
   }
 };
 
-// the two bf16 parts of eight values
-__device__ __forceinline__ void split(const float (&a)[8], u32x4& hi, u32x4& lo) {
+// The three bf16 parts of eight values: the upper half of a value's word, of what is left of it, and of what is left then.  They are cut
+// and not rounded: each difference is exact, and the largest values do not round to an infinity.
+__device__ __forceinline__ void split(const float (&a)[8], bf16x8 (&part)[3]) {
+  u32x4 w[3];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    hi[i] = pack_bf16x2(a[2 * i], a[2 * i + 1]);
-    lo[i] = pack_bf16x2(a[2 * i] - __uint_as_float(hi[i] << 16), a[2 * i + 1] - __uint_as_float(hi[i] & 0xFFFF0000u));
+    float x[2] = {a[2 * i], a[2 * i + 1]};
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      w[k][i] = __builtin_amdgcn_perm(__float_as_uint(x[1]), __float_as_uint(x[0]), 0x07060302u);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) x[j] -= __uint_as_float(__float_as_uint(x[j]) & 0xFFFF0000u);
+    }
   }
+#pragma unroll
+  for (int k = 0; k < 3; ++k) part[k] = __builtin_bit_cast(bf16x8, w[k]);
 }
 
 // acc[j] += a (8 values of a row of the left operand per lane) * rows, for the four columns j
 __device__ __forceinline__ void mma_rows8(const float (&a)[8], const Rows8<bf16_t>& rows, f32x16 (&acc)[4]) {
-  u32x4 hi, lo;
-  split(a, hi, lo);
-  const bf16x8 h8 = __builtin_bit_cast(bf16x8, hi), l8 = __builtin_bit_cast(bf16x8, lo);
+  bf16x8 part[3];
+  split(a, part);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const bf16x8 b = rows.operand(j);
-    acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(h8, b, acc[j], 0, 0, 0);
-    acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(l8, b, acc[j], 0, 0, 0);
-  }
+  for (int k = 0; k < 3; ++k)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(part[k], rows.operand(j), acc[j], 0, 0, 0);
 }
 __device__ __forceinline__ void mma_rows8(const float (&a)[8], const Rows8<float>& rows, f32x16 (&acc)[4]) {
 #pragma unroll
@@ -126,6 +133,15 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const T* base, int row
 }
 constexpr uint32_t kNoColumn = 0xF0000000u;   // an offset behind the rows of any tile, also with a row's offset added
 
+// A step of 16 blocks of ds in LDS, 128 words of 16 bytes: put as four blocks 4 q .. 4 q + 3 (q < 4) of a token, got as the eight of
+// its lane's row of the left operand.
+__device__ __forceinline__ void put_ds(u32x4* step, int row, int q, u32x4 x) { step[(q & 1) * 64 + (q >> 1) * 32 + row] = x; }
+__device__ __forceinline__ void get_ds(const u32x4* step, int lane, float (&x)[8]) {
+  const u32x4 w[2] = {step[lane], step[64 + lane]};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i / 4][i % 4]);
+}
+
 // A step of 16 blocks of the router in LDS, as the matrix instructions want it: kUnits words of 16 bytes per lane.
 template <typename T>
 struct StepWords;
@@ -136,27 +152,18 @@ struct StepWords<bf16_t> {
 #pragma unroll
     for (int j = 0; j < 4; ++j) lds[j * 64 + lane] = __builtin_bit_cast(u32x4, w.operand(j));
   }
-  // four values of ds, blocks 4 q .. 4 q + 3 (q < 4) of a step, into the left operand's words: high parts, then low parts
-  static __device__ __forceinline__ void put_ds(u32x4* step, int row, int q, u32x4 x) {
-    u32x2 hi, lo;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float a = __uint_as_float(x[2 * i]), b = __uint_as_float(x[2 * i + 1]);
-      hi[i] = pack_bf16x2(a, b);
-      lo[i] = pack_bf16x2(a - __uint_as_float(hi[i] << 16), b - __uint_as_float(hi[i] & 0xFFFF0000u));
-    }
-    u32x2* at = reinterpret_cast<u32x2*>(step + (q >> 1) * 32 + row) + (q & 1);
-    at[0] = hi;
-    at[128] = lo;
-  }
   static __device__ __forceinline__ void mma(const u32x4* step, const u32x4* lds, int lane, f32x16 (&acc)[4]) {
-    const u32x4 hi = step[lane], lo = step[64 + lane];
+    float x[8];
+    get_ds(step, lane, x);
+    bf16x8 part[3];
+    split(x, part);
+    bf16x8 b[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const bf16x8 b = __builtin_bit_cast(bf16x8, lds[j * 64 + lane]);
-      acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, hi), b, acc[j], 0, 0, 0);
-      acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, lo), b, acc[j], 0, 0, 0);
-    }
+    for (int j = 0; j < 4; ++j) b[j] = __builtin_bit_cast(bf16x8, lds[j * 64 + lane]);
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(part[k], b[j], acc[j], 0, 0, 0);
   }
 };
 template <>
@@ -166,14 +173,14 @@ struct StepWords<float> {
 #pragma unroll
     for (int u = 0; u < 8; ++u) lds[u * 64 + lane] = __builtin_bit_cast(u32x4, w.w[u]);
   }
-  static __device__ __forceinline__ void put_ds(u32x4* step, int row, int q, u32x4 x) { step[(q & 1) * 64 + (q >> 1) * 32 + row] = x; }
   static __device__ __forceinline__ void mma(const u32x4* step, const u32x4* lds, int lane, f32x16 (&acc)[4]) {
-    const u32x4 x[2] = {step[lane], step[64 + lane]};
+    float x[8];
+    get_ds(step, lane, x);
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       const f32x4 b = __builtin_bit_cast(f32x4, lds[u * 64 + lane]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x[u / 4][u % 4]), b[j], acc[j], 0, 0, 0);
+      for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[u], b[j], acc[j], 0, 0, 0);
     }
   }
 };
@@ -252,7 +259,7 @@ __device__ __forceinline__ void route_dh(const RouteGradArgs<T>& a, int along, i
     for (int i = 0; i < kAhead / 2; ++i) {
       wave_lds_fence();
 #pragma unroll
-      for (int k = 0; k < 4; ++k) Words::put_ds(s_ds + (lane >> 2 & 1) * 128, 8 * k + (lane >> 3), lane & 3, x[i][k]);
+      for (int k = 0; k < 4; ++k) put_ds(s_ds + (lane >> 2 & 1) * 128, 8 * k + (lane >> 3), lane & 3, x[i][k]);
       load_ds(next, next_s0 + 2 * i, x[i]);
       wave_lds_fence();
       if (real) {
