@@ -464,6 +464,8 @@ meft_status meft_balance_bwd(const meft_shape* shape, const meft_balance* balanc
  *   dWg      [n_blocks, d] out  may be NULL
  *   dbias    [n_blocks] f32 out may be NULL
  * bf16 shapes multiply three bf16 parts of dscores, which together hold its 24 bits: dscores is not rounded.
+ * An infinity or NaN in dscores, h, Wg or add makes the elements that it enters infinite or NaN, with factors of 0 too, and no
+ * others: the rows of h have to be finite also where they only pad the batch.
  */
 meft_status meft_route_bwd(const meft_shape* shape, const void* h, const void* Wg, const float* dscores, const void* add, void* dh,
                            void* dWg, float* dbias, void* ws, size_t ws_bytes, void* stream);
