@@ -332,7 +332,8 @@ meft_status meft_adam_rows(const meft_shape* shape, const meft_adam* hp, void* W
  * not used, flags included: all operands are device memory.  `ws` is a device workspace of meft_block_workspace_bytes(shape)
  * bytes, 256-byte aligned; nothing in it outlives a call.  No call allocates, synchronises or uses floating-point atomics:
  * results are identical from run to run, and every call can be captured into a HIP graph.  All sums are accumulated in fp32, and each
- * result is rounded once, when it is stored.  Outputs must not overlap inputs except where it is said.  [T, d] operands are
+ * result is rounded once, when it is stored.  Outputs must not overlap inputs or each other except where it is said (then from the
+ * first byte on); meft_norm_bwd, meft_add_norm_bwd and meft_route_bwd refuse it with MEFT_ERR_INVALID_ARG.  [T, d] operands are
  * 16-byte aligned; so are [d] and [T, n_blocks] ones; the others need the alignment of their type.
  * With T == 0 nothing is read but the outputs that are sums over tokens are written (zeros).
  */

@@ -1,6 +1,7 @@
 // Host side of the calls around the layer (include/meft.h): norms, dropout, the router's balance loss and its gradient.
 // Argument validation, workspace layout and launches; the kernels are in the headers included below.
 #include <cmath>
+#include <initializer_list>
 #include <mutex>
 
 #include "balance.h"
@@ -18,6 +19,31 @@ template <typename T>
 bool aligned_as(const void* p) { return reinterpret_cast<uintptr_t>(p) % alignof(T) == 0; }
 bool ok16(const void* p) { return p && aligned16(p); }
 bool null_or16(const void* p) { return !p || aligned16(p); }
+
+// An operand's bytes.  Outputs share none with each other or with an input that is read while they are written; one that the
+// header lets stand in an input's place starts where it does.
+struct Span {
+  const void* p;
+  size_t bytes;
+  bool shares(const Span& o) const {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(o.p);
+    return p && o.p && bytes && o.bytes && (a < b ? b - a < bytes : a - b < o.bytes);
+  }
+};
+// the first `in_place` of the outputs may stand in the place of one of `places`
+bool outputs_apart(std::initializer_list<Span> outs, int in_place, std::initializer_list<Span> ins, std::initializer_list<Span> places) {
+  int i = 0;
+  for (const Span* o = outs.begin(); o != outs.end(); ++o, ++i) {
+    for (const Span* other = outs.begin(); other != o; ++other)
+      if (o->shares(*other)) return false;
+    for (const Span& in : ins)
+      if (o->shares(in)) return false;
+    for (const Span& in : places)
+      if (o->shares(in) && (i >= in_place || o->p != in.p)) return false;
+  }
+  return true;
+}
+size_t row_bytes(const meft_shape& s) { return (size_t)s.d * (s.dtype == MEFT_BF16 ? 2 : 4); }
 
 // ---- norms ----------------------------------------------------------------------------------
 // Groups of eight columns per lane and waves per row: two groups where they spare waves, and with them barriers, as far as the
@@ -382,6 +408,9 @@ meft_status meft_norm_bwd(const meft_shape* shape, const meft_norm* norm, const 
     return MEFT_ERR_INVALID_ARG;
   if (!aligned_as<float>(mean) || (norm->kind == MEFT_NORM_LAYER && !mean)) return MEFT_ERR_INVALID_ARG;
   if ((rc = check_block_ws(s, ws, ws_bytes)) != MEFT_OK) return rc;
+  const size_t vec = row_bytes(s), rows = vec * s.T, stat = (size_t)s.T * 4;
+  if (!outputs_apart({{dx, rows}, {dgamma, vec}, {dbeta, vec}}, 1, {{x, rows}, {gamma, vec}, {mean, stat}, {rstd, stat}}, {{dh, rows}, {dy, rows}}))
+    return MEFT_ERR_INVALID_ARG;
   hipStream_t st = static_cast<hipStream_t>(stream);
   MEFT_API_LOCK();
   clear_stale_error();
@@ -450,6 +479,10 @@ meft_status meft_add_norm_bwd(const meft_shape* shape, const meft_norm* norm, co
     return MEFT_ERR_INVALID_ARG;
   if (!aligned_as<float>(mean) || (norm->kind == MEFT_NORM_LAYER && !mean)) return MEFT_ERR_INVALID_ARG;
   if ((rc = check_block_ws(s, ws, ws_bytes)) != MEFT_OK) return rc;
+  const size_t vec = row_bytes(s), rows = vec * s.T, stat = (size_t)s.T * 4;
+  if (!outputs_apart({{dres, rows}, {dout, rows}, {dgamma, vec}, {dbeta, vec}}, 2, {{y, rows}, {gamma, vec}, {mean, stat}, {rstd, stat}},
+                     {{dh, rows}, {dy, rows}}))
+    return MEFT_ERR_INVALID_ARG;
   hipStream_t st = static_cast<hipStream_t>(stream);
   MEFT_API_LOCK();
   clear_stale_error();
@@ -513,6 +546,9 @@ meft_status meft_route_bwd(const meft_shape* shape, const void* h, const void* W
       !(dh || dWg || dbias) || (add && !dh))
     return MEFT_ERR_INVALID_ARG;
   if ((rc = check_block_ws(s, ws, ws_bytes)) != MEFT_OK) return rc;
+  const size_t rows = row_bytes(s) * s.T, router = row_bytes(s) * s.n_blocks, bias = (size_t)s.n_blocks * 4;
+  if (!outputs_apart({{dh, rows}, {dWg, router}, {dbias, bias}}, 1, {{h, rows}, {Wg, router}, {dscores, bias * s.T}}, {{add, rows}}))
+    return MEFT_ERR_INVALID_ARG;
   hipStream_t st = static_cast<hipStream_t>(stream);
   MEFT_API_LOCK();
   clear_stale_error();
