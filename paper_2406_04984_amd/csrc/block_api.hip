@@ -82,9 +82,10 @@ int norm_bwd_grid(const meft_shape& s) {
   return norm_grid(s, eight < kCus ? kCus : eight < 2 * kCus ? (int)eight : 2 * kCus);
 }
 // Few rows: the weights' gradients apart, in one launch with dx.  Forward + backward, us, apart / two launches: 128 x 768 fp32 13.1 /
-// 16.3, 512 x 768 fp32 12.3 / 15.3, 512 x 4096 bf16 14.4 / 16.1; 1000 x 4096 22.0 / 19.3, and 1000 x 768 fp32 14.9 / 15.9 with
+// 16.3, 512 x 768 fp32 12.3 / 15.3, 512 x 4096 bf16 14.4 / 16.1; wider rows 16 x 8192 bf16 12.7 / 16.4, 512 x 8192 bf16 18.4 / 20.5,
+// 512 x 8192 fp32 29.5 / 30.3, 512 x 16384 fp32 61.5 / 98.3; more rows 1000 x 4096 22.0 / 19.3, and 1000 x 768 fp32 14.9 / 15.9 with
 // 10.9 us on the device instead of 8.9.
-bool norm_columns_apart(const meft_shape& s) { return s.T > 0 && s.T <= 512 && s.d <= 4096; }
+bool norm_columns_apart(const meft_shape& s) { return s.T > 0 && s.T <= 512; }
 int norm_apart_rows(const meft_shape& s) {
   const int slots = norm_max_slots(norm_shape(s.d).w);
   return (int)(((int64_t)s.T + slots - 1) / slots);
