@@ -245,7 +245,6 @@ __global__ __launch_bounds__((balance_threads<Z, W>())) void balance_part_kernel
 __global__ __launch_bounds__(1024) void balance_join_kernel(BalancePart part, int n_part, int B, int e, BalanceOut out) {
   __shared__ float s_prob[16][64], s_lse2[16];
   __shared__ int32_t s_cnt[16][64], s_tok[16];
-  __shared__ uint32_t s_last;
   const int tid = threadIdx.x, lane = tid & 63, g = tid >> 6, b = blockIdx.x * 64 + lane;
   float p = 0.f, l2 = 0.f;
   int32_t c = 0, n = 0;
