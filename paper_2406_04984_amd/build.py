@@ -34,11 +34,11 @@ def _finish(procs, verbose):
         raise RuntimeError("hipcc failed")
 
 
-def build_library(verbose: bool = True, sources=None) -> str:
-    """Compiles the sources side by side and links them.  `sources`: only these anew, the others' objects as they are."""
+def build_library(verbose: bool = True) -> str:
+    """Compiles the sources side by side and links them."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     objects = {s: os.path.splitext(s)[0] + ".o" for s in SOURCES}
-    _finish([_start([hipcc, *FLAGS, "-c", "-o", objects[s], s], verbose) for s in sources or SOURCES], verbose)
+    _finish([_start([hipcc, *FLAGS, "-c", "-o", o, s], verbose) for s, o in objects.items()], verbose)
     _finish([_start([hipcc, *FLAGS, "-shared", "-o", LIB, *objects.values()], verbose)], verbose)
     return LIB
 
