@@ -82,8 +82,7 @@ __device__ __forceinline__ void store8(T* p, const float (&v)[8], bool past) {
   Vec8<T>::store(p, v);
 }
 
-constexpr int kDropGroups = 1;                    // groups of eight columns per thread and round
-constexpr int kDropSpan = 256 * kDropGroups;      // of a workgroup
+constexpr int kDropSpan = 256;   // groups of eight columns of a workgroup and round, one a thread
 
 // Memory bounds it: 20 integer multiplications per eight elements hide behind their 32 to 48 bytes.  8192 x 4096 bf16, p 0.05:
 // 37 us with a residual (5.4 TB/s; 42 with the result kept in L2), 25.7 without (5.2 TB/s); four groups a thread in a grid that
@@ -97,41 +96,29 @@ __global__ __launch_bounds__(256) void dropout_add_kernel(const T* out, const T*
   uint64_t first = (uint64_t)blockIdx.x * kDropSpan;
   uint32_t t0 = (uint32_t)(first / (uint32_t)groups), g0 = (uint32_t)(first % (uint32_t)groups);
   const uint64_t offset = kDrop ? drop_offset(a) : 0;
-  Raw8<T> raw_out[kDropGroups], raw_res[kDropGroups];
+  Raw8<T> raw_out, raw_res;
   auto load = [&](uint64_t at) {
-#pragma unroll
-    for (int u = 0; u < kDropGroups; ++u) {
-      const uint64_t i = at + u * 256 + threadIdx.x;
-      if (i >= total) continue;
-      raw_out[u].load(out + i * 8);
-      if (res) raw_res[u].load(res + i * 8);
-    }
+    const uint64_t i = at + threadIdx.x;
+    if (i >= total) return;
+    raw_out.load(out + i * 8);
+    if (res) raw_res.load(res + i * 8);
   };
-#pragma unroll
-  for (int u = 0; u < kDropGroups; ++u) {
-    raw_out[u].clear();
-    raw_res[u].clear();
-  }
+  raw_out.clear();
+  raw_res.clear();
   load(first);
   for (; first < total; first += stride) {
-    float v[kDropGroups][8], r[kDropGroups][8];
-#pragma unroll
-    for (int u = 0; u < kDropGroups; ++u) {
-      raw_out[u].widen(v[u]);
-      raw_res[u].widen(r[u]);
-    }
+    float v[8], r[8];
+    raw_out.widen(v);
+    raw_res.widen(r);
     load(first + stride);
-#pragma unroll
-    for (int u = 0; u < kDropGroups; ++u) {
-      const uint64_t i = first + u * 256 + threadIdx.x;
-      if (kDrop) {
-        const uint32_t w = g0 + u * 256 + threadIdx.x, dt = (uint32_t)tile_div((int)w, groups, inv);
-        drop8(a, offset, t0 + dt, w - dt * groups, v[u]);
-      }
-#pragma unroll
-      for (int z = 0; z < 8; ++z) v[u][z] += r[u][z];
-      if (i < total) store8(y + i * 8, v[u], past);
+    const uint64_t i = first + threadIdx.x;
+    if (kDrop) {
+      const uint32_t w = g0 + threadIdx.x, dt = (uint32_t)tile_div((int)w, groups, inv);
+      drop8(a, offset, t0 + dt, w - dt * groups, v);
     }
+#pragma unroll
+    for (int z = 0; z < 8; ++z) v[z] += r[z];
+    if (i < total) store8(y + i * 8, v, past);
     t0 += step_t;
     g0 += step_g;
     if (g0 >= (uint32_t)groups) {
