@@ -354,9 +354,11 @@ typedef struct {
  * mask again.  Element (t, c) takes 16 bits of Philox4x32 with 10 rounds, counter (c / 8, t, low word, high word of offset),
  * key (low word, high word of seed): word (c % 8) / 2 of the result, its low half for even c; it stays where they are at least
  * round(65536 p), and is then multiplied by 65536 / (65536 - round(65536 p)).  The mask of a token does not depend on T or d.
- * offset: one value for each layer and step, so that masks differ; where `step` (device memory, 8-byte aligned, may be NULL) is
- * given, the value it holds when the kernel runs is added to offset (modulo 2^64): a captured step draws anew when the program
- * changes it between replays.  p in [0, 1) and round(65536 p) <= 65535; below 2^-17 nothing is dropped.
+ * offset: one value for each layer and step, so that masks differ.  Ranks of data-parallel training count their tokens from 0 each:
+ * they need a seed or an offset of their own as well, or their different tokens get the same mask.  Where `step` (device memory,
+ * 8-byte aligned, may be NULL) is given, the value it holds when the kernel runs is added to offset (modulo 2^64): a captured step
+ * draws anew when the program changes it between replays (a counter of steps there, and the layer in offset's high word, never
+ * meet).  p in [0, 1) and round(65536 p) <= 65535; below 2^-17 nothing is dropped.
  */
 typedef struct {
   float p;
