@@ -7,8 +7,11 @@
 // The counts carry no gradient (a selection has none).  A row of scores that are all -inf counts as a token that is not
 // valid: it has no softmax.
 //
-// W waves hold a row in registers, Z scores per lane; W = 1 up to 1024 blocks.  What bounds it are a row's vector instructions and,
-// for few rows, the launches.  16384 x 256: partial sums 7 us, their join 5.5, the gradient 10 (33 MB); 2048 x 64: 3.9, 3.2, 3.3.
+// W waves hold a row in registers, Z scores per lane; W = 1 up to 1024 blocks.  16384 x 256: partial sums 7.5 us, their join
+// 5.5, the gradient 10.1 (17, 0.5 and 34 MB); 2048 x 64: 3.9, 3.3, 3.2.  Neither memory (5.2 TB/s would be 3.2 and 6.5 us) nor the
+// vector instructions alone bound the large ones: by the counters a row takes 135 and 171 of these, which keep the vector units busy
+// for 3.8 and 4.8 us, and the waves spend 60 % of their time waiting, with one row each asked for ahead.  For few rows it is the
+// launches.
 #pragma once
 #include "common.h"
 

@@ -397,7 +397,7 @@ __global__ __launch_bounds__(64 * W * norm_max_slots(W)) void norm_bwd_kernel(No
 }
 
 // dgamma and dbeta (blockIdx.y) from the workgroups' partial sums: 8 threads along 32 columns, 64 along the workgroups.  Bound by
-// one or two round trips to memory: 4.4 us for 512 workgroups of 4096 columns (16 columns a workgroup 4.9; a loop over the
+// one or two round trips to memory: 5.1 us for 512 workgroups of 4096 columns (16 columns a workgroup 5.7; a loop over the
 // workgroups that does not ask ahead 8 to 10).
 template <typename T>
 __global__ __launch_bounds__(512) void norm_grad_kernel(const float* __restrict__ part, int n_part, int d, T* dgamma, T* dbeta) {

@@ -79,7 +79,8 @@ __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
 // blocks l, l + 64, ... in registers; e rounds of a wave-wide maximum through DPP moves, its lowest block by ballots,
 // and the winner is retired by zeroing its key (a live key is never 0 for finite scores).  Output order: score
 // descending, block id ascending.  Against keys in LDS and 64-bit shuffles: 8.7 -> 5 us (8192 tokens, 64 blocks).
-// kKeep: the scores themselves are written too.
+// kKeep: the scores themselves are written too (us a call, without / with: 8192 x 4096, 64 blocks 23.0 / 23.2, 16384 x 1024, 256 blocks
+// 47.2 / 50.0).
 template <int Z, bool kKeep>
 __global__ __launch_bounds__(256) void route_pick_kernel(const float* __restrict__ p, int n_part, size_t part_stride,
                                                          const float* __restrict__ bias, int n_tok, int B, int e,

@@ -8,11 +8,11 @@
 // (it wants eight rows of one column per lane); lane l then holds columns 4 (l % 32) + j of its four result tiles j, so that a
 // result row leaves as one 8- or 16-byte word per lane, 32 lanes on consecutive addresses.
 //
-// 8192 x 4096 bf16, 64 blocks: 48.5 us for 217 MB (4.5 TB/s; a copy in tiles of this shape reaches 5.0 to 5.3) and 5.1 for the join;
+// 8192 x 4096 bf16, 64 blocks: 49 us for 217 MB (4.4 TB/s; a copy in tiles of this shape reaches 5.0 to 5.3) and 5.0 for the join;
 // 4096 x 4096, 256 blocks: 67 and 8 us, there bound by the instructions of dWg's waves and by their loads through the vector cache.
 //
 // ds arrives in fp32.  bf16 shapes cut it in three bf16 parts of eight bits each, which together are ds (below 2^-110 up to the last bits
-// that bf16's range has), and multiply all three: the products are those of fp32.  Two parts take 50.5 and 55 us there and keep 16 bits.
+// that bf16's range has), and multiply all three: the products are those of fp32.  Two parts took 47 and 53 us there and kept 16 bits.
 // fp32 shapes use fp32 matrix instructions.
 #pragma once
 #include "common.h"

@@ -11,7 +11,7 @@ namespace meft {
 // B scores sits in LDS as ordered keys; e rounds of a wave-wide arg-max, the winner is retired
 // by zeroing its key (a live key is never 0 for finite scores).  Output order: score descending,
 // block id ascending.  The scores may arrive as n_part partial sums, part_stride floats apart.
-// kKeep: the scores themselves are written too.
+// kKeep: the scores themselves are written too (16384 tokens, 1024 blocks, us a call, without / with: 213 / 227).
 // ---------------------------------------------------------------------------------------------
 template <bool kKeep>
 __global__ __launch_bounds__(64) void route_topk_kernel(const float* __restrict__ p, int n_part, size_t part_stride,
