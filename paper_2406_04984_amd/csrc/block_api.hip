@@ -409,8 +409,8 @@ meft_status meft_norm_bwd(const meft_shape* shape, const meft_norm* norm, const 
     return MEFT_ERR_INVALID_ARG;
   if (!aligned_as<float>(mean) || (norm->kind == MEFT_NORM_LAYER && !mean)) return MEFT_ERR_INVALID_ARG;
   if ((rc = check_block_ws(s, ws, ws_bytes)) != MEFT_OK) return rc;
-  const size_t vec = row_bytes(s), rows = vec * s.T, stat = (size_t)s.T * 4;
-  if (!outputs_apart({{dx, rows}, {dgamma, vec}, {dbeta, vec}}, 1, {{x, rows}, {gamma, vec}, {mean, stat}, {rstd, stat}}, {{dh, rows}, {dy, rows}}))
+  const size_t vec = row_bytes(s), rows = vec * s.T, stat = (size_t)s.T * 4, means = norm->kind == MEFT_NORM_LAYER ? stat : 0;
+  if (!outputs_apart({{dx, rows}, {dgamma, vec}, {dbeta, vec}}, 1, {{x, rows}, {gamma, vec}, {mean, means}, {rstd, stat}}, {{dh, rows}, {dy, rows}}))
     return MEFT_ERR_INVALID_ARG;
   hipStream_t st = static_cast<hipStream_t>(stream);
   MEFT_API_LOCK();
@@ -480,8 +480,8 @@ meft_status meft_add_norm_bwd(const meft_shape* shape, const meft_norm* norm, co
     return MEFT_ERR_INVALID_ARG;
   if (!aligned_as<float>(mean) || (norm->kind == MEFT_NORM_LAYER && !mean)) return MEFT_ERR_INVALID_ARG;
   if ((rc = check_block_ws(s, ws, ws_bytes)) != MEFT_OK) return rc;
-  const size_t vec = row_bytes(s), rows = vec * s.T, stat = (size_t)s.T * 4;
-  if (!outputs_apart({{dres, rows}, {dout, rows}, {dgamma, vec}, {dbeta, vec}}, 2, {{y, rows}, {gamma, vec}, {mean, stat}, {rstd, stat}},
+  const size_t vec = row_bytes(s), rows = vec * s.T, stat = (size_t)s.T * 4, means = norm->kind == MEFT_NORM_LAYER ? stat : 0;
+  if (!outputs_apart({{dres, rows}, {dout, rows}, {dgamma, vec}, {dbeta, vec}}, 2, {{y, rows}, {gamma, vec}, {mean, means}, {rstd, stat}},
                      {{dh, rows}, {dy, rows}}))
     return MEFT_ERR_INVALID_ARG;
   hipStream_t st = static_cast<hipStream_t>(stream);

@@ -28,9 +28,10 @@ def _main(rec_path):
         sp = ctypes.byref(_Shape(T, D, NB * 8, NB, 8, 2, 1, 0, 0, 0))
         at = {n: (i + 1) << 40 for i, n in enumerate(ARGS[call])}      # far apart
         own = dict(at)
+        rms = places.pop("rms", False)
         for n, where in places.items():
             at[n] = None if where is None else own[where[0]] + where[1]
-        norm, drop = ctypes.byref(_Norm(0, 1e-5)), ctypes.byref(_Drop(0.1, 1, 2))
+        norm, drop = ctypes.byref(_Norm(int(rms), 1e-5)), ctypes.byref(_Drop(0.1, 1, 2))
         head = {"norm_bwd": (norm,), "add_norm_bwd": (norm, drop, vp(None)), "route_bwd": ()}[call]
         rec.rec_clear()
         rc = getattr(lib, "meft_" + call)(sp, *head, *[vp(at[n]) for n in ARGS[call]], vp(1 << 50),
@@ -54,7 +55,7 @@ REFUSED = [
     (16, "norm_bwd", {"dx": ("x", 256)}), (16, "norm_bwd", {"dx": ("x", 16 - 16 * 256)}), (16, "norm_bwd", {"dx": ("dh", 256)}),
     (16, "norm_bwd", {"dx": ("dy", -256)}), (16, "norm_bwd", {"dgamma": ("gamma", 0)}), (16, "norm_bwd", {"dbeta": ("gamma", 240)}),
     (16, "norm_bwd", {"dbeta": ("dgamma", 0)}), (16, "norm_bwd", {"dgamma": ("dx", 256)}), (16, "norm_bwd", {"dgamma": ("dh", 0)}),
-    (16, "norm_bwd", {"dx": ("rstd", 48)}), (16, "add_norm_bwd", {"dres": ("y", 0)}), (16, "add_norm_bwd", {"dout": ("y", 15 * 256)}),
+    (16, "norm_bwd", {"dx": ("rstd", 48)}), (16, "norm_bwd", {"dx": ("mean", 48)}), (16, "add_norm_bwd", {"dres": ("y", 0)}), (16, "add_norm_bwd", {"dout": ("y", 15 * 256)}),
     (16, "add_norm_bwd", {"dout": ("dres", 256)}), (16, "add_norm_bwd", {"dout": ("dh", 512)}), (16, "add_norm_bwd", {"dgamma": ("gamma", 0)}),
     (16, "route_bwd", {"dh": ("h", 0)}), (16, "route_bwd", {"dh": ("h", 256), "add": None}), (16, "route_bwd", {"dh": ("add", 256)}),
     (16, "route_bwd", {"dh": ("dscores", 0)}), (16, "route_bwd", {"dh": ("Wg", 3 * 256)}), (16, "route_bwd", {"dWg": ("Wg", 0)}),
@@ -69,6 +70,8 @@ ALLOWED = [
     (16, "add_norm_bwd", {"dres": ("dy", 0), "dout": ("dh", 0)}), (16, "route_bwd", {}), (16, "route_bwd", {"dh": ("add", 0)}),
     (16, "route_bwd", {"dh": ("h", 16 * 256)}), (16, "route_bwd", {"dWg": ("Wg", -4 * 256)}), (16, "route_bwd", {"dh": None, "add": None}),
     (16, "route_bwd", {"dWg": None, "dbias": None}),
+    # the mean of the rms kind is not read
+    (16, "norm_bwd", {"rms": True, "mean": ("dx", 0)}), (16, "add_norm_bwd", {"rms": True, "mean": ("dout", 64)}),
     # no token, no row that could be overwritten
     (0, "norm_bwd", {"dx": ("x", 0)}), (0, "add_norm_bwd", {"dres": ("y", 0)}), (0, "route_bwd", {"dh": ("h", 0)}),
 ]
